@@ -354,6 +354,140 @@ simsd_status simsd_verify_accept_lmhead(const simsd_lmhead_desc* desc, const voi
                                         size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Rotary positions, and the write into the cache                             */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Shape of one rotary call on tokens packed back to back.  Element (i, h, c) of
+ * x in {q, k, v, q_out, k_out} is x[i*x_stride_token + h*x_stride_head + c]: the
+ * parts of a fused projection's output are passed as they lie.  Strides are in
+ * elements, non-negative, at most 2^40 and multiples of 16 bytes; those of an
+ * output must keep its rows apart.  The cache fields are those of
+ * simsd_attn_desc; simsd_rotary ignores them.
+ */
+typedef struct {
+  int32_t num_tokens;         /* rows of q, k, v and the outputs, 0..2^24          */
+  int32_t num_q_heads;        /* Hq >= 0 (0: no queries, q and q_out NULL)         */
+  int32_t num_kv_heads;       /* Hkv >= 0 (0: no keys; simsd_rotary only)          */
+  int32_t head_dim;           /* a multiple of 8, 8..512                          */
+  int32_t rotary_dim;         /* leading dims of a head that turn: even,
+                                 2..head_dim; the rest is copied                  */
+  int32_t interleaved;        /* 0: dims i and i + rotary_dim/2 pair;
+                                 1: dims 2i and 2i + 1 pair                       */
+  int32_t batch;              /* append: sequences, 1..65535                      */
+  int32_t max_kv_len;         /* append: cache indices written are < this, >= 0    */
+  int32_t page_size;          /* append: 0 = contiguous cache; else tokens per page */
+  int32_t max_pages_per_seq;  /* append, paged: block_table row length,
+                                 >= ceil(max_kv_len / page_size)                  */
+  int32_t num_pages;          /* append, paged: pages in the pool, >= 0            */
+  float attn_factor;          /* multiplies the rotated values; finite, > 0
+                                 (1 unless the frequencies are scaled by "yarn")   */
+  int64_t q_stride_token, q_stride_head;
+  int64_t k_stride_token, k_stride_head;
+  int64_t v_stride_token, v_stride_head;         /* append */
+  int64_t q_out_stride_token, q_out_stride_head;
+  int64_t k_out_stride_token, k_out_stride_head; /* simsd_rotary */
+  int64_t cache_stride_seq, cache_stride_token, cache_stride_head;
+  simsd_dtype dtype;          /* of q, k, v, the outputs and the cache            */
+} simsd_rotary_desc;
+
+/*
+ * Rotary embedding: pair i < rotary_dim/2 of token t's heads,
+ *   (x1, x2) -> attn_factor * (x1 cos a - x2 sin a, x2 cos a + x1 sin a),
+ *   a = positions[t] * freq[i],
+ * with the angle formed and reduced in fp64 and the rotation in fp32, rounded
+ * once to `dtype`.  The verification step's new slots take their RoPE-copy
+ * positions (simsd_verify_attention then gets rope_theta = 0); this call
+ * serves the layouts and scaled frequencies that the fused rotation lacks.
+ *
+ *   q          [num_tokens, Hq, head_dim], or NULL if Hq == 0
+ *   k          [num_tokens, Hkv, head_dim], or NULL if Hkv == 0
+ *   positions  [num_tokens] int32 (any value)
+ *   freq       [rotary_dim/2] float64, radians a position (device memory;
+ *              simsd_rope_frequencies fills a host copy)
+ *   q_out, k_out  like q and k; each may be its input itself, with the same
+ *              strides (in place), and otherwise overlaps no input
+ * All data pointers are 16-byte aligned.  One kernel; no workspace.
+ */
+simsd_status simsd_rotary(const simsd_rotary_desc* desc, const void* q, const void* k,
+                          const int32_t* positions, const double* freq, void* q_out, void* k_out,
+                          void* stream);
+
+/*
+ * The same rotation for the new tokens of a ragged batch, with the rotated keys
+ * and the values written to the cache that simsd_verify_attention and
+ * simsd_chunk_attention read.  Tokens q_starts[b] <= t < q_starts[b+1] belong to
+ * sequence b and take the cache indices kv_lens[b] - n_b .. kv_lens[b] - 1 in
+ * order (n_b of them: kv_lens counts the new tokens).
+ *
+ *   q_starts   [batch + 1] int32, not falling, at most num_tokens; rows of
+ *              tokens before q_starts[0] or from q_starts[batch] on are left as
+ *              they were
+ *   kv_lens    [batch] int32 cached length of each sequence, new tokens included
+ *   positions  [num_tokens] int32, or NULL: a token's position is its cache index
+ *   v          [num_tokens, Hkv, head_dim], written to v_cache unchanged
+ *   q, q_out   may both be NULL (Hq == 0) where only the cache is filled
+ *   block_table [batch, max_pages_per_seq] int32, or NULL if page_size == 0
+ * A token whose cache index is outside [0, max_kv_len), or whose page id is
+ * outside [0, num_pages), is not written to the cache (its query still turns).
+ * Two tokens that take one cache row leave either's values there.
+ */
+simsd_status simsd_rotary_append(const simsd_rotary_desc* desc, const void* q, const void* k,
+                                 const void* v, const int32_t* positions, const double* freq,
+                                 void* q_out, void* k_cache, void* v_cache,
+                                 const int32_t* block_table, const int32_t* q_starts,
+                                 const int32_t* kv_lens, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Sampling                                                                   */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+  int32_t rows;              /* rows of logits, 0..2^21                            */
+  int32_t vocab;             /* V, 1..2^22                                         */
+  float temperature;         /* T, finite and >= 0 (0: the largest logit)          */
+  int32_t top_k;             /* >= 0; 0 or >= V: off                               */
+  float top_p;               /* 0..1; 1: off                                       */
+  float min_p;               /* 0..1; 0: off                                       */
+  simsd_dtype dtype;         /* of logits                                          */
+} simsd_sample_desc;
+
+/*
+ * One token for each row of logits (the drafter's proposals, or the target's
+ * own tokens where nothing was drafted).  With m the row's largest logit,
+ * w_i = exp((x_i - m) / T), and tokens in the order of falling logits, the
+ * lowest index first among equal ones (-0 == +0):
+ *   top_k   keeps the first k tokens;
+ *   top_p   of those, the fewest leading ones whose weights add up to top_p of
+ *           all theirs or more (at least one);
+ *   min_p   keeps the tokens with w_i >= min_p;
+ * and the token is the first kept one, in that order, at which the running
+ * weight exceeds u times the weight of all kept tokens, u = uniforms[row].
+ * Logits of -inf or NaN, and those more than 700 T below m, are never kept.
+ * If m is +inf, only the logits of +inf are.  T <= 0 (or NaN) selects the first
+ * token of the order.  A row that keeps nothing gives token -1.  The random
+ * numbers are the caller's, and the running sums are exact to 1e-8 of the
+ * largest weight and the same on every run.
+ *
+ *   logits       [rows, V], aligned to their elements
+ *   uniforms     [rows] float32 in [0, 1)
+ *   temperatures, top_ks, top_ps, min_ps   [rows] float32 / int32, or NULL: the
+ *                descriptor's value for every row.  In these, top_k <= 0,
+ *                top_p >= 1 or NaN and min_p <= 0 or NaN are off, top_p <= 0
+ *                keeps the first token, min_p >= 1 those equal to it, and an
+ *                infinite temperature is the largest finite one
+ *   token        [rows] int32
+ *   prob         [rows] float32 the token's weight over that of all kept tokens
+ *                (0 for token -1), or NULL
+ *   kept         [rows] int32 number of kept tokens, or NULL
+ * One kernel; no workspace.
+ */
+simsd_status simsd_sample(const simsd_sample_desc* desc, const void* logits, const float* uniforms,
+                          const float* temperatures, const int32_t* top_ks, const float* top_ps,
+                          const float* min_ps, int32_t* token, float* prob, int32_t* kept,
+                          void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Host-only helpers (no GPU needed)                                          */
 /* ------------------------------------------------------------------------ */
 
@@ -364,6 +498,28 @@ simsd_status simsd_verify_accept_lmhead(const simsd_lmhead_desc* desc, const voi
  * sequence in simsd_last_error(). */
 simsd_status simsd_validate_step_map(const int32_t* step_map_host, const int32_t* num_ref_host,
                                      int32_t batch, int32_t block_size, int32_t max_ref);
+
+/* Frequencies of the rotary pairs, and the factor on the rotated values, for a
+ * context scaled to `factor` times the original one:
+ *   NONE    f_i = theta^(-2i/rotary_dim)
+ *   LINEAR  f_i / factor (positions interpolated)
+ *   NTK     the base grown to theta * factor^(rotary_dim / (rotary_dim - 2))
+ *   YARN    pairs that turn beta_fast times or more in the original context keep
+ *           f_i, those that turn beta_slow times or less take f_i / factor, and
+ *           those between are blended linearly in the pair index, between the
+ *           indices of beta_fast (rounded down) and beta_slow (rounded up);
+ *           *attn_factor = 0.1 ln(factor) + 1
+ * `freq` [rotary_dim/2] and `attn_factor` are host memory; original_context and
+ * the betas matter to YARN only. */
+typedef enum {
+  SIMSD_ROPE_NONE = 0,
+  SIMSD_ROPE_LINEAR = 1,
+  SIMSD_ROPE_NTK = 2,
+  SIMSD_ROPE_YARN = 3
+} simsd_rope_scaling;
+simsd_status simsd_rope_frequencies(int32_t rotary_dim, double theta, simsd_rope_scaling scaling,
+                                    double factor, int32_t original_context, double beta_fast,
+                                    double beta_slow, double* freq, float* attn_factor);
 
 const char* simsd_status_string(simsd_status status);
 const char* simsd_last_error(void); /* message of this thread's last failed call */

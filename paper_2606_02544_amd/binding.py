@@ -48,6 +48,24 @@ class LmheadDesc(ctypes.Structure):
                 ("hidden", ctypes.c_int32), ("dtype", ctypes.c_int)]
 
 
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("num_tokens", "num_q_heads", "num_kv_heads", "head_dim", "rotary_dim", "interleaved",
+                 "batch", "max_kv_len", "page_size", "max_pages_per_seq", "num_pages")] + \
+               [("attn_factor", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in
+                ("q_stride_token", "q_stride_head", "k_stride_token", "k_stride_head",
+                 "v_stride_token", "v_stride_head", "q_out_stride_token", "q_out_stride_head",
+                 "k_out_stride_token", "k_out_stride_head", "cache_stride_seq",
+                 "cache_stride_token", "cache_stride_head")] + [("dtype", ctypes.c_int)]
+
+
+class SampleDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
 class SimsdError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -88,6 +106,17 @@ def lib() -> ctypes.CDLL:
         L.simsd_verify_accept_lmhead.argtypes = [ctypes.POINTER(LmheadDesc)] + [_P] * 9 + \
             [_P, ctypes.c_size_t, _P]
         L.simsd_verify_accept_lmhead.restype = ctypes.c_int
+        L.simsd_rotary.argtypes = [ctypes.POINTER(RotaryDesc)] + [_P] * 7
+        L.simsd_rotary.restype = ctypes.c_int
+        L.simsd_rotary_append.argtypes = [ctypes.POINTER(RotaryDesc)] + [_P] * 12
+        L.simsd_rotary_append.restype = ctypes.c_int
+        L.simsd_rope_frequencies.argtypes = [ctypes.c_int32, ctypes.c_double, ctypes.c_int,
+                                             ctypes.c_double, ctypes.c_int32, ctypes.c_double,
+                                             ctypes.c_double, ctypes.POINTER(ctypes.c_double),
+                                             ctypes.POINTER(ctypes.c_float)]
+        L.simsd_rope_frequencies.restype = ctypes.c_int
+        L.simsd_sample.argtypes = [ctypes.POINTER(SampleDesc)] + [_P] * 10
+        L.simsd_sample.restype = ctypes.c_int
         L.simsd_validate_step_map.argtypes = [_I32P, _I32P, ctypes.c_int32, ctypes.c_int32,
                                               ctypes.c_int32]
         L.simsd_validate_step_map.restype = ctypes.c_int
@@ -604,3 +633,245 @@ def validate_step_map(step_map, num_ref, max_ref: int):
     nr = np.ascontiguousarray(num_ref, dtype=np.int32)
     _check(lib().simsd_validate_step_map(sm.ctypes.data_as(_I32P), nr.ctypes.data_as(_I32P),
                                          sm.shape[0], sm.shape[1], max_ref))
+
+
+# ----------------------------------------------------------------------------
+# Operators beside the verification step: rotary positions and the write into
+# the cache, sampling.  Their tests format no message for arguments that pass.
+# New outputs are allocated on the call's stream.
+# ----------------------------------------------------------------------------
+def _raise(msg: str):
+    raise ValueError(msg)
+
+
+class _Launch:
+    """Where a call runs: `handle` is the stream's, and inside the context the
+    tensors' device and (when the caller gave one) the stream are current, for
+    the launch and for new outputs."""
+
+    def __init__(self, device: torch.device, stream):
+        if device.type != "cuda":
+            _raise(f"tensors must be on a GPU, got {device}")
+        self._contexts = []
+        if stream is not None:
+            if stream.device != device:
+                _raise(f"stream is on {stream.device}, tensors are on {device}")
+            self.handle = stream.cuda_stream
+            if stream != torch.cuda.current_stream(device):
+                self._contexts.append(torch.cuda.stream(stream))
+        else:
+            self.handle = torch.cuda.current_stream(device).cuda_stream
+        if torch.cuda.current_device() != device.index:
+            self._contexts.append(torch.cuda.device(device))
+
+    def __enter__(self):
+        for c in self._contexts:
+            c.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        for c in reversed(self._contexts):
+            c.__exit__(*exc)
+
+
+def _heads(name: str, t, shape, dtype, device):
+    """t is [tokens, heads, d] of this shape, dtype and device with a unit
+    stride over d; returns its (token, head) strides (0 where there is one)."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        _raise(f"{name} must be a 3-D tensor [tokens, heads, d]")
+    if t.shape != shape:
+        _raise(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype is not dtype:
+        _raise(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        _raise(f"{name} is on {t.device}, expected {device}")
+    st = t.stride()
+    if st[2] != 1:
+        _raise(f"{name} must have a unit stride over the head dimension")
+    return (st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0)
+
+
+def _vector(name: str, t, n: int, dtype, device):
+    if not (isinstance(t, torch.Tensor) and _is(t, (n,), dtype, device)):
+        _tensor(name, t, (n,), dtype, device)
+
+
+@functools.lru_cache(maxsize=1024)
+def _rotary_desc(*fields) -> RotaryDesc:
+    return RotaryDesc(*fields)
+
+
+def _rotary_parts(q, k, freq):
+    """Tokens, (Hq, Hkv), d, dtype and device of a rotary call's inputs, and
+    the rotary dims its frequencies turn."""
+    x = q if q is not None else k
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        _raise("q (or k) must be a 3-D tensor [tokens, heads, d]")
+    if x.dtype is not torch.bfloat16 and x.dtype is not torch.float32:
+        _raise(f"q and k must be bfloat16 or float32, got {x.dtype}")
+    if not isinstance(freq, torch.Tensor) or freq.dim() != 1:
+        _raise("freq must be a 1-D tensor [rotary_dim / 2]")
+    _vector("freq", freq, freq.shape[0], torch.float64, x.device)
+    return x.shape[0], x.shape[2], x.dtype, x.device, 2 * freq.shape[0]
+
+
+def rope_frequencies(rotary_dim: int, theta: float, *, scaling: str = "none", factor: float = 1.0,
+                     original_context: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                     device="cuda"):
+    """simsd_rope_frequencies: (freq, attn_factor) for rotary and rotary_append,
+    freq a float64 tensor [rotary_dim / 2] on `device`.  scaling is "none",
+    "linear", "ntk" or "yarn"."""
+    kinds = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+    if scaling not in kinds:
+        _raise(f"scaling must be one of {sorted(kinds)}, got {scaling!r}")
+    n = operator.index(rotary_dim)
+    freq = torch.empty(max(n, 2) // 2, dtype=torch.float64)
+    attn_factor = ctypes.c_float()
+    _check(lib().simsd_rope_frequencies(
+        n, theta, kinds[scaling], factor, operator.index(original_context), beta_fast, beta_slow,
+        ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double)), ctypes.byref(attn_factor)))
+    return freq.to(device), attn_factor.value
+
+
+def rotary(q, k, positions, freq, *, interleaved: bool = False, attn_factor: float = 1.0,
+           q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """simsd_rotary on torch tensors: q [tokens, Hq, d] and k [tokens, Hkv, d]
+    (either may be None) turned by positions [tokens] (int32), freq as from
+    rope_frequencies.  Inputs and outputs may be strided over tokens and heads;
+    q_out=q or k_out=k turns in place.  Returns (q_out, k_out)."""
+    T, d, dt, dev, rot = _rotary_parts(q, k, freq)
+    strides = []
+    heads = []
+    outs = []
+    for name, x, out in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            if out is not None:
+                _raise(f"{name}_out without {name}")
+            strides += [0, 0, 0, 0]
+            heads.append(0)
+            outs.append(None)
+            continue
+        if not isinstance(x, torch.Tensor) or x.dim() != 3:
+            _raise(f"{name} must be a 3-D tensor [tokens, heads, d]")
+        shape = (T, x.shape[1], d)
+        strides += _heads(name, x, shape, dt, dev)
+        heads.append(shape[1])
+        strides += _heads(name + "_out", out, shape, dt, dev) if out is not None else \
+            (shape[1] * d if T > 1 else 0, d if shape[1] > 1 else 0)
+        outs.append(out)
+    _vector("positions", positions, T, torch.int32, dev)
+    with _Launch(dev, stream) as at:
+        for i, x in enumerate((q, k)):
+            if x is not None and outs[i] is None:
+                outs[i] = torch.empty(x.shape, dtype=dt, device=dev)
+        qs, ks = strides[:4], strides[4:]
+        desc = _rotary_desc(T, heads[0], heads[1], d, rot, int(bool(interleaved)), 0, 0, 0, 0, 0,
+                            float(attn_factor), qs[0], qs[1], ks[0], ks[1], 0, 0, qs[2], qs[3],
+                            ks[2], ks[3], 0, 0, 0, _dtype_code(dt))
+        _check(lib().simsd_rotary(ctypes.byref(desc), _addr(q), _addr(k), positions.data_ptr(),
+                                  freq.data_ptr(), _addr(outs[0]), _addr(outs[1]), at.handle))
+    return outs[0], outs[1]
+
+
+def _ragged(q_starts, kv_lens, device) -> int:
+    """Sequences of a ragged batch: q_starts [batch + 1], kv_lens [batch]."""
+    if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1 or kv_lens.shape[0] < 1:
+        _raise("kv_lens must be a 1-D tensor [batch]")
+    b = kv_lens.shape[0]
+    _vector("kv_lens", kv_lens, b, torch.int32, device)
+    _vector("q_starts", q_starts, b + 1, torch.int32, device)
+    return b
+
+
+def _cache_strides(k_cache, v_cache, dtype, device, hkv, d, page_size, max_kv_len, batch,
+                   block_table):
+    """Strides and pages per sequence of a call's cache, which passes _check_cache."""
+    if max_kv_len <= 0:
+        return (0, 0, 0), 0
+    _check_cache(k_cache, v_cache, dtype, device, hkv, d, page_size, max_kv_len, batch, block_table)
+    st = k_cache.stride()
+    return st[:3], block_table.shape[1] if page_size > 0 else 0
+
+
+def rotary_append(q, k, v, k_cache, v_cache, block_table, q_starts, kv_lens, freq, *,
+                  max_kv_len: int, page_size: int = 0, positions=None, interleaved: bool = False,
+                  attn_factor: float = 1.0, q_out: Optional[torch.Tensor] = None, stream=None):
+    """simsd_rotary_append on torch tensors: turns q [tokens, Hq, d] (may be
+    None) into q_out and writes the turned k and v [tokens, Hkv, d] to the cache
+    rows of the last q_starts[b+1] - q_starts[b] of each sequence's kv_lens[b]
+    tokens.  Returns q_out (None without q); rows outside q_starts' range are
+    left as they were."""
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        _raise("k must be a 3-D tensor [tokens, Hkv, d]")
+    T, d, dt, dev, rot = _rotary_parts(k, None, freq)
+    hkv, hq = k.shape[1], 0
+    qs, qo = (0, 0), (0, 0)
+    if q is not None:
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            _raise("q must be a 3-D tensor [tokens, Hq, d]")
+        hq = q.shape[1]
+        qs = _heads("q", q, (T, hq, d), dt, dev)
+        qo = (hq * d if T > 1 else 0, d if hq > 1 else 0) if q_out is None else \
+            _heads("q_out", q_out, (T, hq, d), dt, dev)
+    elif q_out is not None:
+        _raise("q_out without q")
+    ks, vs = _heads("k", k, (T, hkv, d), dt, dev), _heads("v", v, (T, hkv, d), dt, dev)
+    b = _ragged(q_starts, kv_lens, dev)
+    page_size, max_kv_len = operator.index(page_size), operator.index(max_kv_len)
+    cs, pages = _cache_strides(k_cache, v_cache, dt, dev, hkv, d, page_size, max_kv_len, b, block_table)
+    if max_kv_len > 0 and any(n > 1 and st == 0 for n, st in zip(k_cache.shape, k_cache.stride())):
+        _raise("the cache must not be an expanded tensor: its rows are written")
+    if positions is not None:
+        _vector("positions", positions, T, torch.int32, dev)
+    with _Launch(dev, stream) as at:
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        desc = _rotary_desc(T, hq, hkv, d, rot, int(bool(interleaved)), b, max_kv_len, page_size, pages,
+                            k_cache.shape[0] if pages else 0, float(attn_factor), qs[0], qs[1],
+                            ks[0], ks[1], vs[0], vs[1], qo[0], qo[1], 0, 0, cs[0], cs[1], cs[2],
+                            _dtype_code(dt))
+        _check(lib().simsd_rotary_append(
+            ctypes.byref(desc), _addr(q), k.data_ptr(), v.data_ptr(), _addr(positions),
+            freq.data_ptr(), _addr(q_out), _addr(k_cache), _addr(v_cache),
+            _addr(block_table if pages else None), q_starts.data_ptr(), kv_lens.data_ptr(), at.handle))
+    return q_out
+
+
+@functools.lru_cache(maxsize=1024)
+def _sample_desc(*fields) -> SampleDesc:
+    return SampleDesc(*fields)
+
+
+def sample(logits, uniforms, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None,
+           prob=None, kept=None, stream=None):
+    """simsd_sample on torch tensors: one token for each row of logits [rows, V],
+    drawn by uniforms [rows] (float32).  temperature, top_p and min_p are numbers
+    or float32 tensors [rows], top_k a number or an int32 tensor [rows].
+    Returns (token, prob, kept)."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        _raise("logits must be a 2-D tensor [rows, V]")
+    dt, dev, (n, V) = logits.dtype, logits.device, logits.shape
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        _raise(f"logits must be bfloat16 or float32, got {dt}")
+    if not logits.is_contiguous():
+        _raise("logits must be contiguous")
+    _vector("uniforms", uniforms, n, torch.float32, dev)
+    rows = [None] * 4
+    numbers = [temperature, top_k, top_p, min_p]
+    for i, (name, kind, off) in enumerate((("temperature", torch.float32, 1.0), ("top_k", torch.int32, 0),
+                                           ("top_p", torch.float32, 1.0), ("min_p", torch.float32, 0.0))):
+        x = numbers[i]
+        if isinstance(x, torch.Tensor):
+            _vector(name, x, n, kind, dev)
+            rows[i], numbers[i] = x, off
+        else:
+            numbers[i] = operator.index(x) if kind is torch.int32 else float(x)
+    with _Launch(dev, stream) as at:
+        token = _given("token", token, (n,), torch.int32, dev)
+        prob = _given("prob", prob, (n,), torch.float32, dev)
+        kept = _given("kept", kept, (n,), torch.int32, dev)
+        desc = _sample_desc(n, V, *numbers, _dtype_code(dt))
+        _check(lib().simsd_sample(ctypes.byref(desc), logits.data_ptr(), uniforms.data_ptr(),
+                                  *map(_addr, rows), token.data_ptr(), prob.data_ptr(),
+                                  kept.data_ptr(), at.handle))
+    return token, prob, kept

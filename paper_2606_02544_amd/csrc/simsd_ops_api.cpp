@@ -1,0 +1,146 @@
+// extern "C" entry points of the operators beside the verification step:
+// check, plan, fill the argument block, launch.
+#include <hip/hip_runtime.h>
+
+#include <string>
+
+#include "simsd.h"
+#include "simsd_kernels.h"
+#include "simsd_ops_kernels.h"
+#include "simsd_ops_plan.h"
+
+using namespace simsd;
+
+static simsd_status hip_fail(hipError_t e, const char* what) {
+  set_error(std::string(what) + ": " + hipGetErrorString(e));
+  return SIMSD_ERR_HIP;
+}
+
+static RotaryArgs rotary_args(const simsd_rotary_desc* d, const RotaryPlan& p) {
+  RotaryArgs a{};
+  a.tokens = d->num_tokens;
+  a.hq = d->num_q_heads;
+  a.hkv = d->num_kv_heads;
+  a.d = d->head_dim;
+  a.rot = d->rotary_dim;
+  a.q_tok = d->q_stride_token;
+  a.q_head = d->q_stride_head;
+  a.k_tok = d->k_stride_token;
+  a.k_head = d->k_stride_head;
+  a.v_tok = d->v_stride_token;
+  a.v_head = d->v_stride_head;
+  a.qo_tok = d->q_out_stride_token;
+  a.qo_head = d->q_out_stride_head;
+  a.ko_tok = d->k_out_stride_token;
+  a.ko_head = d->k_out_stride_head;
+  a.cs_seq = d->cache_stride_seq;
+  a.cs_tok = d->cache_stride_token;
+  a.cs_head = d->cache_stride_head;
+  a.batch = d->batch;
+  a.page_size = d->page_size;
+  a.max_pages = d->max_pages_per_seq;
+  a.num_pages = d->num_pages;
+  a.max_kv = d->max_kv_len;
+  a.q_units = p.q_units;
+  a.v_units = p.v_units;
+  a.units = p.units;
+  a.factor = d->attn_factor;
+  return a;
+}
+
+extern "C" simsd_status simsd_rotary(const simsd_rotary_desc* desc, const void* q, const void* k,
+                                     const int32_t* positions, const double* freq, void* q_out,
+                                     void* k_out, void* stream) {
+  try {
+    RotaryPlan p;
+    simsd_status st = plan_rotary(desc, false, &p);
+    if (st == SIMSD_OK) st = check_rotary_args(desc, q, k, positions, freq, q_out, k_out);
+    if (st != SIMSD_OK || desc->num_tokens == 0) return st;
+    int dev = 0, cus = 0;
+    const hipError_t qe = stream_device(stream, &dev, &cus);
+    if (qe != hipSuccess) return hip_fail(qe, "simsd_rotary: device query");
+    RotaryArgs a = rotary_args(desc, p);
+    a.q = q;
+    a.k = k;
+    a.positions = positions;
+    a.freq = freq;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    const hipError_t e = launch_rotary(*desc, p, a, false, cus, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "simsd_rotary launch");
+    return SIMSD_OK;
+  } catch (...) {
+    set_error("simsd_rotary: internal error");
+    return SIMSD_ERR_HIP;
+  }
+}
+
+extern "C" simsd_status simsd_rotary_append(const simsd_rotary_desc* desc, const void* q,
+                                            const void* k, const void* v, const int32_t* positions,
+                                            const double* freq, void* q_out, void* k_cache,
+                                            void* v_cache, const int32_t* block_table,
+                                            const int32_t* q_starts, const int32_t* kv_lens,
+                                            void* stream) {
+  try {
+    RotaryPlan p;
+    simsd_status st = plan_rotary(desc, true, &p);
+    if (st == SIMSD_OK)
+      st = check_rotary_append_args(desc, q, k, v, freq, q_out, k_cache, v_cache, block_table,
+                                    q_starts, kv_lens);
+    if (st != SIMSD_OK || desc->num_tokens == 0) return st;
+    int dev = 0, cus = 0;
+    const hipError_t qe = stream_device(stream, &dev, &cus);
+    if (qe != hipSuccess) return hip_fail(qe, "simsd_rotary_append: device query");
+    RotaryArgs a = rotary_args(desc, p);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.positions = positions;
+    a.freq = freq;
+    a.q_out = q_out;
+    a.k_out = k_cache;
+    a.v_out = v_cache;
+    a.block_table = block_table;
+    a.q_starts = q_starts;
+    a.kv_lens = kv_lens;
+    const hipError_t e = launch_rotary(*desc, p, a, true, cus, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "simsd_rotary_append launch");
+    return SIMSD_OK;
+  } catch (...) {
+    set_error("simsd_rotary_append: internal error");
+    return SIMSD_ERR_HIP;
+  }
+}
+
+extern "C" simsd_status simsd_sample(const simsd_sample_desc* desc, const void* logits,
+                                     const float* uniforms, const float* temperatures,
+                                     const int32_t* top_ks, const float* top_ps, const float* min_ps,
+                                     int32_t* token, float* prob, int32_t* kept, void* stream) {
+  try {
+    SampleArgs a{};
+    simsd_status st = plan_sample(desc, &a.one);
+    if (st == SIMSD_OK)
+      st = check_sample_args(desc, logits, uniforms, temperatures, top_ks, top_ps, min_ps, token, prob, kept);
+    if (st != SIMSD_OK || desc->rows == 0) return st;
+    a.logits = logits;
+    a.uniforms = uniforms;
+    a.temperatures = temperatures;
+    a.top_ks = top_ks;
+    a.top_ps = top_ps;
+    a.min_ps = min_ps;
+    a.token = token;
+    a.prob = prob;
+    a.kept = kept;
+    a.V = desc->vocab;
+    a.temperature = desc->temperature;
+    a.top_p = desc->top_p;
+    a.min_p = desc->min_p;
+    a.top_k = desc->top_k;
+    const hipError_t e = launch_sample(*desc, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "simsd_sample launch");
+    return SIMSD_OK;
+  } catch (...) {
+    set_error("simsd_sample: internal error");
+    return SIMSD_ERR_HIP;
+  }
+}

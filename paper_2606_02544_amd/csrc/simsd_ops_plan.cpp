@@ -1,0 +1,232 @@
+// Planning, argument checking and host helpers of the operators beside the
+// verification step.  No HIP calls: this file is plain C++17.
+#include "simsd_ops_plan.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <string>
+
+#include "simsd_plan.h"
+
+namespace simsd {
+
+static simsd_status fail(simsd_status st, const std::string& msg) {
+  set_error(msg);
+  return st;
+}
+
+static bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A dtype field as the integer a C caller stored there.
+static bool known_dtype(const simsd_dtype& field) {
+  int v;
+  std::memcpy(&v, &field, sizeof v);
+  return v == SIMSD_F32 || v == SIMSD_BF16;
+}
+
+static simsd_status check_strides(const char* op, const int64_t* s, int n, int eb, int most_log2) {
+  for (int i = 0; i < n; ++i) {
+    if (s[i] < 0) return fail(SIMSD_ERR_BAD_SHAPE, std::string(op) + ": negative stride");
+    if (s[i] % (16 / eb) != 0)
+      return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": strides must be multiples of 16 bytes");
+    if (s[i] > (int64_t{1} << most_log2))
+      return fail(SIMSD_ERR_BAD_SHAPE,
+                  std::string(op) + ": stride beyond 2^" + std::to_string(most_log2) + " elements");
+  }
+  return SIMSD_OK;
+}
+
+// Rows [tokens, heads] of d elements that do not overlap, whichever index is outer.
+// (Strides up to 2^40 times counts up to 2^31: 128-bit products.)
+static bool apart(__int128 tokens, __int128 heads, __int128 st, __int128 sh, __int128 d) {
+  if (tokens < 1 || heads < 1) return true;
+  const bool head_inner = (heads == 1 || sh >= d) && (tokens == 1 || st >= sh * (heads - 1) + d);
+  const bool token_inner = (tokens == 1 || st >= d) && (heads == 1 || sh >= st * (tokens - 1) + d);
+  return head_inner || token_inner;
+}
+
+simsd_status plan_rotary(const simsd_rotary_desc* d, bool append, RotaryPlan* p) {
+  if (!d || !p) return fail(SIMSD_ERR_NULL_POINTER, "rotary: descriptor is NULL");
+  if (!known_dtype(d->dtype))
+    return fail(SIMSD_ERR_UNSUPPORTED, "rotary: dtype must be SIMSD_F32 or SIMSD_BF16");
+  if (d->num_tokens < 0 || d->num_tokens > (1 << 24))
+    return fail(SIMSD_ERR_BAD_SHAPE, "rotary: num_tokens must be in [0, 2^24]");
+  if (d->num_q_heads < 0 || d->num_kv_heads < 0 || d->num_q_heads > 65535 || d->num_kv_heads > 65535 ||
+      (append && d->num_kv_heads < 1))
+    return fail(SIMSD_ERR_BAD_SHAPE, append ? "rotary: need num_q_heads in [0, 65535] and num_kv_heads in [1, 65535]"
+                                            : "rotary: need num_q_heads and num_kv_heads in [0, 65535]");
+  if (d->head_dim < 8 || d->head_dim > 512 || d->head_dim % 8 != 0)
+    return fail(SIMSD_ERR_UNSUPPORTED, "rotary: head_dim must be a multiple of 8 in [8, 512]");
+  if (d->rotary_dim < 2 || d->rotary_dim > d->head_dim || d->rotary_dim % 2 != 0)
+    return fail(SIMSD_ERR_BAD_SHAPE, "rotary: rotary_dim must be even and in [2, head_dim]");
+  if (d->interleaved != 0 && d->interleaved != 1)
+    return fail(SIMSD_ERR_BAD_SHAPE, "rotary: interleaved must be 0 or 1");
+  if (!(std::isfinite(d->attn_factor) && d->attn_factor > 0.f))
+    return fail(SIMSD_ERR_BAD_SHAPE, "rotary: attn_factor must be finite and > 0");
+  const int eb = d->dtype == SIMSD_F32 ? 4 : 2;
+  const int64_t in[8] = {d->q_stride_token, d->q_stride_head, d->k_stride_token, d->k_stride_head,
+                         d->q_out_stride_token, d->q_out_stride_head,
+                         append ? d->v_stride_token : d->k_out_stride_token,
+                         append ? d->v_stride_head : d->k_out_stride_head};
+  simsd_status st = check_strides("rotary", in, 8, eb, 40);
+  if (st != SIMSD_OK) return st;
+  if (!apart(d->num_tokens, d->num_q_heads, d->q_out_stride_token, d->q_out_stride_head, d->head_dim) ||
+      (!append && !apart(d->num_tokens, d->num_kv_heads, d->k_out_stride_token, d->k_out_stride_head, d->head_dim)))
+    return fail(SIMSD_ERR_BAD_SHAPE, "rotary: rows of an output overlap");
+  if (append) {
+    if (d->batch < 1 || d->batch > 65535)
+      return fail(SIMSD_ERR_BAD_SHAPE, "rotary: batch must be in [1, 65535]");
+    if (d->max_kv_len < 0) return fail(SIMSD_ERR_BAD_SHAPE, "rotary: max_kv_len < 0");
+    if (d->page_size < 0) return fail(SIMSD_ERR_BAD_SHAPE, "rotary: page_size < 0");
+    if (d->page_size > 0 && (d->num_pages < 0 || d->max_pages_per_seq < ceil_div(d->max_kv_len, d->page_size)))
+      return fail(SIMSD_ERR_BAD_SHAPE,
+                  "rotary: need num_pages >= 0 and max_pages_per_seq >= ceil(max_kv_len / page_size)");
+    const int64_t cache[3] = {d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head};
+    st = check_strides("rotary", cache, 3, eb, 48);
+    if (st != SIMSD_OK) return st;
+  }
+  RotaryPlan r;
+  // Vectors of 16 bytes where both halves of the turning part (or, interleaved,
+  // the part itself) are whole vectors; single elements else.
+  const int w = 16 / eb, half = d->rotary_dim / 2;
+  r.vec = (d->interleaved ? d->rotary_dim : half) % w == 0 ? w : 1;
+  const int copy = (d->head_dim - d->rotary_dim) / r.vec;
+  r.q_units = (d->interleaved ? (r.vec > 1 ? d->rotary_dim / r.vec : half) : half / r.vec) + copy;
+  r.v_units = append ? d->head_dim / w : 0;
+  const int64_t units = int64_t{r.q_units} * (int64_t{d->num_q_heads} + d->num_kv_heads) +
+                        int64_t{r.v_units} * d->num_kv_heads;
+  if (units > (int64_t{1} << 26)) return fail(SIMSD_ERR_BAD_SHAPE, "rotary: too many heads");
+  r.units = static_cast<int>(units);
+  *p = r;
+  return SIMSD_OK;
+}
+
+simsd_status check_rotary_args(const simsd_rotary_desc* d, const void* q, const void* k,
+                               const int32_t* positions, const double* freq, const void* q_out,
+                               const void* k_out) {
+  if (d->num_tokens == 0) return SIMSD_OK;
+  if (!positions || !freq) return fail(SIMSD_ERR_NULL_POINTER, "rotary: positions and freq are required");
+  if ((d->num_q_heads > 0 && (!q || !q_out)) || (d->num_kv_heads > 0 && (!k || !k_out)))
+    return fail(SIMSD_ERR_NULL_POINTER, "rotary: q, q_out (Hq > 0) and k, k_out (Hkv > 0) are required");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16))
+    return fail(SIMSD_ERR_ALIGNMENT, "rotary: q, k and the outputs must be 16-byte aligned");
+  if (!aligned(positions, 4) || !aligned(freq, 8))
+    return fail(SIMSD_ERR_ALIGNMENT, "rotary: positions must be 4-byte and freq 8-byte aligned");
+  if ((d->num_q_heads > 0 && q == q_out && (d->q_stride_token != d->q_out_stride_token || d->q_stride_head != d->q_out_stride_head)) ||
+      (d->num_kv_heads > 0 && k == k_out && (d->k_stride_token != d->k_out_stride_token || d->k_stride_head != d->k_out_stride_head)))
+    return fail(SIMSD_ERR_BAD_SHAPE, "rotary: an output in place needs its input's strides");
+  return SIMSD_OK;
+}
+
+simsd_status check_rotary_append_args(const simsd_rotary_desc* d, const void* q, const void* k,
+                                      const void* v, const double* freq, const void* q_out,
+                                      const void* k_cache, const void* v_cache,
+                                      const int32_t* block_table, const int32_t* q_starts,
+                                      const int32_t* kv_lens) {
+  if (d->num_tokens == 0) return SIMSD_OK;
+  if (!k || !v || !freq || !q_starts || !kv_lens)
+    return fail(SIMSD_ERR_NULL_POINTER, "rotary: k, v, freq, q_starts and kv_lens are required");
+  if (d->num_q_heads > 0 && (!q || !q_out))
+    return fail(SIMSD_ERR_NULL_POINTER, "rotary: q and q_out are required (Hq > 0)");
+  if (d->max_kv_len > 0 && (!k_cache || !v_cache))
+    return fail(SIMSD_ERR_NULL_POINTER, "rotary: k_cache and v_cache are required");
+  if (d->page_size > 0 && d->max_kv_len > 0 && !block_table)
+    return fail(SIMSD_ERR_NULL_POINTER, "rotary: block_table required for a paged cache");
+  const void* data[] = {q, k, v, q_out, k_cache, v_cache};
+  for (const void* a : data)
+    if (!aligned(a, 16))
+      return fail(SIMSD_ERR_ALIGNMENT, "rotary: q, k, v, q_out and the cache must be 16-byte aligned");
+  if (!aligned(freq, 8)) return fail(SIMSD_ERR_ALIGNMENT, "rotary: freq must be 8-byte aligned");
+  if (d->num_q_heads > 0 && q == q_out &&
+      (d->q_stride_token != d->q_out_stride_token || d->q_stride_head != d->q_out_stride_head))
+    return fail(SIMSD_ERR_BAD_SHAPE, "rotary: q_out in place needs the strides of q");
+  return SIMSD_OK;
+}
+
+simsd_status plan_sample(const simsd_sample_desc* d, double* one) {
+  if (!d || !one) return fail(SIMSD_ERR_NULL_POINTER, "sample: descriptor is NULL");
+  if (!known_dtype(d->dtype))
+    return fail(SIMSD_ERR_UNSUPPORTED, "sample: dtype must be SIMSD_F32 or SIMSD_BF16");
+  if (d->rows < 0 || d->rows > (1 << 21)) return fail(SIMSD_ERR_BAD_SHAPE, "sample: rows must be in [0, 2^21]");
+  if (d->vocab < 1 || d->vocab > (1 << 22)) return fail(SIMSD_ERR_BAD_SHAPE, "sample: vocab must be in [1, 2^22]");
+  if (!(std::isfinite(d->temperature) && d->temperature >= 0.f))
+    return fail(SIMSD_ERR_BAD_SHAPE, "sample: temperature must be finite and >= 0");
+  if (d->top_k < 0) return fail(SIMSD_ERR_BAD_SHAPE, "sample: top_k must be >= 0");
+  if (!(d->top_p >= 0.f && d->top_p <= 1.f) || !(d->min_p >= 0.f && d->min_p <= 1.f))
+    return fail(SIMSD_ERR_BAD_SHAPE, "sample: top_p and min_p must be in [0, 1]");
+  int bits = 0;                                  // ceil(log2 V): V weights of 2^(62 - bits) stay below 2^63
+  while ((int64_t{1} << bits) < d->vocab) ++bits;
+  *one = std::ldexp(1.0, 62 - bits);
+  return SIMSD_OK;
+}
+
+simsd_status check_sample_args(const simsd_sample_desc* d, const void* logits, const float* uniforms,
+                               const float* temperatures, const int32_t* top_ks, const float* top_ps,
+                               const float* min_ps, const int32_t* token, const float* prob,
+                               const int32_t* kept) {
+  if (d->rows == 0) return SIMSD_OK;
+  if (!logits || !uniforms || !token)
+    return fail(SIMSD_ERR_NULL_POINTER, "sample: logits, uniforms and token are required");
+  if (!aligned(logits, d->dtype == SIMSD_F32 ? 4 : 2))
+    return fail(SIMSD_ERR_ALIGNMENT, "sample: logits must be aligned to their elements");
+  const void* words[] = {uniforms, temperatures, top_ks, top_ps, min_ps, token, prob, kept};
+  for (const void* w : words)
+    if (!aligned(w, 4)) return fail(SIMSD_ERR_ALIGNMENT, "sample: arrays must be 4-byte aligned");
+  return SIMSD_OK;
+}
+
+}  // namespace simsd
+
+using namespace simsd;
+
+extern "C" simsd_status simsd_rope_frequencies(int32_t rotary_dim, double theta,
+                                               simsd_rope_scaling scaling, double factor,
+                                               int32_t original_context, double beta_fast,
+                                               double beta_slow, double* freq, float* attn_factor) {
+  int kind;
+  std::memcpy(&kind, &scaling, sizeof kind);
+  if (!freq || !attn_factor) return fail(SIMSD_ERR_NULL_POINTER, "rope_frequencies: NULL output");
+  if (kind < SIMSD_ROPE_NONE || kind > SIMSD_ROPE_YARN)
+    return fail(SIMSD_ERR_UNSUPPORTED, "rope_frequencies: unknown scaling");
+  if (rotary_dim < 2 || rotary_dim > 512 || rotary_dim % 2 != 0)
+    return fail(SIMSD_ERR_BAD_SHAPE, "rope_frequencies: rotary_dim must be even and in [2, 512]");
+  if (!(std::isfinite(theta) && theta > 1.0))
+    return fail(SIMSD_ERR_BAD_SHAPE, "rope_frequencies: theta must be finite and > 1");
+  if (kind != SIMSD_ROPE_NONE && !(std::isfinite(factor) && factor >= 1.0))
+    return fail(SIMSD_ERR_BAD_SHAPE, "rope_frequencies: factor must be finite and >= 1");
+  if (kind == SIMSD_ROPE_NTK && rotary_dim < 4)
+    return fail(SIMSD_ERR_BAD_SHAPE, "rope_frequencies: NTK scaling needs rotary_dim >= 4");
+  if (kind == SIMSD_ROPE_YARN &&
+      !(original_context >= 1 && std::isfinite(beta_fast) && beta_slow > 0.0 && beta_fast >= beta_slow))
+    return fail(SIMSD_ERR_BAD_SHAPE,
+                "rope_frequencies: YARN needs original_context >= 1 and beta_fast >= beta_slow > 0");
+  const int half = rotary_dim / 2;
+  const double d = rotary_dim;
+  const double base = kind == SIMSD_ROPE_NTK ? theta * std::pow(factor, d / (d - 2.0)) : theta;
+  *attn_factor = 1.f;
+  double low = 0.0, high = 0.0;
+  if (kind == SIMSD_ROPE_YARN) {
+    // Pair index whose pair turns `beta` times in the original context.
+    const double two_pi = 6.283185307179586476925;
+    auto index = [&](double beta) { return d * std::log(original_context / (beta * two_pi)) / (2.0 * std::log(theta)); };
+    low = std::max(std::floor(index(beta_fast)), 0.0);
+    high = std::min(std::ceil(index(beta_slow)), d - 1.0);
+    if (high <= low) high = low + 0.001;   // a step instead of a ramp
+    *attn_factor = static_cast<float>(0.1 * std::log(factor) + 1.0);
+  }
+  for (int i = 0; i < half; ++i) {
+    const double f = std::pow(base, -2.0 * i / d);
+    if (kind == SIMSD_ROPE_LINEAR) {
+      freq[i] = f / factor;
+    } else if (kind == SIMSD_ROPE_YARN) {
+      const double slow = std::min(std::max((i - low) / (high - low), 0.0), 1.0);
+      freq[i] = f / factor * slow + f * (1.0 - slow);
+    } else {
+      freq[i] = f;
+    }
+  }
+  return SIMSD_OK;
+}
