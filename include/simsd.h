@@ -439,6 +439,68 @@ simsd_status simsd_rotary_append(const simsd_rotary_desc* desc, const void* q, c
                                  const int32_t* kv_lens, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Attention of a chunk of new tokens                                         */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Shape of one chunk-attention call: the new tokens of a ragged batch, packed
+ * back to back, over a cache that holds their own keys and values already
+ * (simsd_rotary_append writes them).  Heads, scale and cache layout are those of
+ * simsd_attn_desc.
+ */
+typedef struct {
+  int32_t num_tokens;         /* rows of q and out, 0..2^23                       */
+  int32_t batch;              /* sequences, 1..65535                              */
+  int32_t num_q_heads;        /* Hq >= 1                                          */
+  int32_t num_kv_heads;       /* Hkv >= 1, Hq % Hkv == 0, Hq / Hkv <= 16          */
+  int32_t head_dim;           /* 64 or 128                                        */
+  int32_t max_q_len;          /* most new tokens of a sequence, >= 0 (it chooses
+                                 the kernel; longer sequences are served too)     */
+  int32_t max_kv_len;         /* upper bound of kv_lens[], 0..2^30                */
+  int32_t mask_block;         /* m: a token sees the keys up to the end of its
+                                 block of m positions; 1: causal, 0: all keys     */
+  int32_t page_size;          /* 0 = contiguous cache; else tokens per page       */
+  int32_t max_pages_per_seq;  /* paged: block_table row length,
+                                 >= ceil(max_kv_len / page_size)                  */
+  int32_t kv_chunk;           /* keys per work-group (multiple of 64; fewer where
+                                 a work-group's 2047 pages hold fewer), or 0 =
+                                 library's choice                                 */
+  int64_t cache_stride_seq;   /* elements between sequences (contiguous) / pages  */
+  int64_t cache_stride_token; /* elements between consecutive tokens              */
+  int64_t cache_stride_head;  /* elements between consecutive KV heads            */
+  float scale;                /* softmax scale; 0 = 1/sqrt(head_dim)              */
+  simsd_dtype dtype;          /* of q, the caches and out                         */
+} simsd_chunk_desc;
+
+size_t simsd_chunk_attention_workspace_size(const simsd_chunk_desc* desc);
+
+/*
+ * Block-causal attention of prompts, chunks of prompts and single tokens.  Token
+ * i of the n_b = q_starts[b+1] - q_starts[b] new ones of sequence b sits at
+ * position p = kv_lens[b] - n_b + i and sees the cached keys
+ *   t < min(kv_lens[b], (p / m + 1) * m),   m = mask_block  (all for m = 0),
+ * none if p < 0.  A row that sees no key gives 0 and a log-sum-exp of -inf.
+ * Keys and values a row does not see have no part in it, whatever they hold.
+ *
+ *   q           [num_tokens, Hq, head_dim]  (rotated)
+ *   k_cache, v_cache, block_table           the cache, as in simsd_attn_desc
+ *   q_starts    [batch + 1] int32, not falling, 0..num_tokens; rows of tokens
+ *               before q_starts[0] or from q_starts[batch] on are left as they were
+ *   kv_lens     [batch] int32, 0..max_kv_len, the new tokens included
+ *   out         [num_tokens, Hq, head_dim]
+ *   lse         [Hq, num_tokens] float32 natural-log log-sum-exp, or NULL
+ * The workspace must hold simsd_chunk_attention_workspace_size() bytes (0 where
+ * one work-group takes all keys of a row; a call with less returns
+ * SIMSD_ERR_WORKSPACE).  One kernel, and a second that joins the parts of rows
+ * whose keys were divided.  The order of additions is fixed for a given shape.
+ */
+simsd_status simsd_chunk_attention(const simsd_chunk_desc* desc, const void* q, const void* k_cache,
+                                   const void* v_cache, const int32_t* block_table,
+                                   const int32_t* q_starts, const int32_t* kv_lens, void* out,
+                                   float* lse, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Sampling                                                                   */
 /* ------------------------------------------------------------------------ */
 

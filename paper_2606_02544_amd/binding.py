@@ -60,6 +60,15 @@ class RotaryDesc(ctypes.Structure):
                  "cache_stride_token", "cache_stride_head")] + [("dtype", ctypes.c_int)]
 
 
+class ChunkDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("num_tokens", "batch", "num_q_heads", "num_kv_heads", "head_dim", "max_q_len",
+                 "max_kv_len", "mask_block", "page_size", "max_pages_per_seq", "kv_chunk")] + \
+               [(n, ctypes.c_int64) for n in
+                ("cache_stride_seq", "cache_stride_token", "cache_stride_head")] + \
+               [("scale", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
 class SampleDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
                 ("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
@@ -115,6 +124,11 @@ def lib() -> ctypes.CDLL:
                                              ctypes.c_double, ctypes.POINTER(ctypes.c_double),
                                              ctypes.POINTER(ctypes.c_float)]
         L.simsd_rope_frequencies.restype = ctypes.c_int
+        L.simsd_chunk_attention_workspace_size.argtypes = [ctypes.POINTER(ChunkDesc)]
+        L.simsd_chunk_attention_workspace_size.restype = ctypes.c_size_t
+        L.simsd_chunk_attention.argtypes = [ctypes.POINTER(ChunkDesc)] + [_P] * 9 + \
+            [ctypes.c_size_t, _P]
+        L.simsd_chunk_attention.restype = ctypes.c_int
         L.simsd_sample.argtypes = [ctypes.POINTER(SampleDesc)] + [_P] * 10
         L.simsd_sample.restype = ctypes.c_int
         L.simsd_validate_step_map.argtypes = [_I32P, _I32P, ctypes.c_int32, ctypes.c_int32,
@@ -835,6 +849,72 @@ def rotary_append(q, k, v, k_cache, v_cache, block_table, q_starts, kv_lens, fre
             freq.data_ptr(), _addr(q_out), _addr(k_cache), _addr(v_cache),
             _addr(block_table if pages else None), q_starts.data_ptr(), kv_lens.data_ptr(), at.handle))
     return q_out
+
+
+def chunk_workspace_size(desc: ChunkDesc) -> int:
+    return int(lib().simsd_chunk_attention_workspace_size(ctypes.byref(desc)))
+
+
+@functools.lru_cache(maxsize=1024)
+def _chunk_desc(device: torch.device, *fields):
+    """ChunkDesc of these field values (read only: calls share it) and the
+    workspace bytes of its call on `device`, which is current."""
+    desc = ChunkDesc(*fields)
+    return desc, chunk_workspace_size(desc)
+
+
+def chunk_attention(q, k_cache, v_cache, block_table, q_starts, kv_lens, *, max_q_len: int,
+                    max_kv_len: int, page_size: int = 0, mask_block: int = 1, kv_chunk: int = 0,
+                    scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, want_lse: bool = True,
+                    workspace: Optional[torch.Tensor] = None, stream=None):
+    """simsd_chunk_attention on torch tensors: q [tokens, Hq, d], contiguous, the
+    new tokens of a ragged batch, over a cache that holds their keys and values.
+    Returns (out [tokens, Hq, d], lse [Hq, tokens] or None); rows outside
+    q_starts' range are left as they were.
+
+    Without a caller's workspace a call takes the buffer held for its stream; one
+    that is captured into a graph takes memory of that graph's own."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        _raise("q must be a 3-D tensor [tokens, Hq, d]")
+    (T, hq, d), dt, dev = q.shape, q.dtype, q.device
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        _raise(f"q must be bfloat16 or float32, got {dt}")
+    if not q.is_contiguous():
+        _raise("q must be contiguous")
+    b = _ragged(q_starts, kv_lens, dev)
+    max_q_len, max_kv_len, page_size, mask_block, kv_chunk = map(
+        operator.index, (max_q_len, max_kv_len, page_size, mask_block, kv_chunk))
+    if max_kv_len > 0:
+        if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+            _raise("k_cache must be a 4-D tensor [seq or page, token, Hkv, d]")
+        hkv = k_cache.shape[2]
+    else:
+        hkv = hq
+    cs, pages = _cache_strides(k_cache, v_cache, dt, dev, hkv, d, page_size, max_kv_len, b, block_table)
+    if out is not None:
+        _tensor("out", out, (T, hq, d), dt, dev)
+    if lse is not None:
+        _tensor("lse", lse, (hq, T), torch.float32, dev)
+    with _Launch(dev, stream) as at:
+        if out is None:
+            out = torch.empty(q.shape, dtype=dt, device=dev)
+        if lse is None and want_lse:
+            lse = torch.empty((hq, T), dtype=torch.float32, device=dev)
+        desc, nbytes = _chunk_desc(dev, T, b, hq, hkv, d, max_q_len, max_kv_len, mask_block, page_size,
+                                   pages, kv_chunk, cs[0], cs[1], cs[2], float(scale), _dtype_code(dt))
+        if workspace is not None:
+            _tensor("workspace", workspace, (None,), None, dev)
+        elif nbytes:
+            if torch.cuda.is_current_stream_capturing():
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            else:
+                workspace = WORKSPACES.get(dev, at.handle, "chunk", nbytes)
+        _check(lib().simsd_chunk_attention(
+            ctypes.byref(desc), q.data_ptr(), _addr(k_cache), _addr(v_cache),
+            _addr(block_table if pages else None), q_starts.data_ptr(), kv_lens.data_ptr(),
+            out.data_ptr(), _addr(lse), _addr(workspace), _nbytes(workspace), at.handle))
+    return out, lse
 
 
 @functools.lru_cache(maxsize=1024)

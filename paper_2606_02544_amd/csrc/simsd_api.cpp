@@ -62,7 +62,7 @@ static hipError_t stream_cus(void* stream, int* cus) {
 
 // Compute units of the current device (workspace-size queries have no
 // stream); the nominal count when no device is visible.
-static int current_cus() {
+int simsd::current_cus() {
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess || device_cus(dev, &cus) != hipSuccess) return kNominalCUs;
   return cus;

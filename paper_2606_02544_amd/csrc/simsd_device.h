@@ -73,8 +73,6 @@ __device__ inline int swz(int r) {
     return ((r & 1) ? 2 : 0) ^ ((r & 2) ? 4 : 0) ^ ((r & 4) ? 1 : 0) ^ ((r & 8) ? 2 : 0);
 }
 
-constexpr int kMaxChunkPages = 2048;           // page ids of one key range staged in LDS
-
 // Direct global -> LDS copy of 16 bytes per lane (global_load_lds_dwordx4):
 // lane i's bytes land at LDS byte lds + 16 * i, so one instruction moves 1 KB.
 // It counts in vmcnt like any vector load but the compiler does not track it:

@@ -89,6 +89,7 @@ int lmhead_vocab_tile(int rows);   // vocabulary entries per scan work-group, by
 // compute units, queried once per device; on failure *cus is an MI355X's 256
 // and the error is returned for the caller to report after validation.
 hipError_t stream_device(void* stream, int* dev, int* cus);
+int current_cus();         // compute units of the current device; nominal when none is visible
 int lmhead_stage();        // reduction elements per stage (H must be a multiple)
 
 }  // namespace simsd

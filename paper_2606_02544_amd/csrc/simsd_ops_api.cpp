@@ -2,6 +2,7 @@
 // check, plan, fill the argument block, launch.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <string>
 
 #include "simsd.h"
@@ -108,6 +109,66 @@ extern "C" simsd_status simsd_rotary_append(const simsd_rotary_desc* desc, const
     return SIMSD_OK;
   } catch (...) {
     set_error("simsd_rotary_append: internal error");
+    return SIMSD_ERR_HIP;
+  }
+}
+
+extern "C" size_t simsd_chunk_attention_workspace_size(const simsd_chunk_desc* desc) {
+  ChunkPlan p;
+  if (plan_chunk(desc, current_cus(), &p) != SIMSD_OK) return 0;
+  return p.workspace;
+}
+
+extern "C" simsd_status simsd_chunk_attention(const simsd_chunk_desc* desc, const void* q,
+                                              const void* k_cache, const void* v_cache,
+                                              const int32_t* block_table, const int32_t* q_starts,
+                                              const int32_t* kv_lens, void* out, float* lse,
+                                              void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    int dev = 0, cus = 0;
+    const hipError_t qe = stream_device(stream, &dev, &cus);
+    ChunkPlan p;
+    simsd_status st = plan_chunk(desc, cus, &p);
+    if (st == SIMSD_OK)
+      st = check_chunk_args(desc, p, q, k_cache, v_cache, block_table, q_starts, kv_lens, out, lse,
+                            workspace, workspace_bytes);
+    if (st != SIMSD_OK || desc->num_tokens == 0) return st;
+    if (qe != hipSuccess) return hip_fail(qe, "simsd_chunk_attention: device query");
+    ChunkArgs a{};
+    a.q = q;
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    a.block_table = desc->page_size > 0 ? block_table : nullptr;
+    a.q_starts = q_starts;
+    a.kv_lens = kv_lens;
+    a.out = out;
+    a.lse = lse;
+    a.part = static_cast<float*>(workspace);
+    a.part_ml = p.workspace ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.ml_off) : nullptr;
+    a.cs_seq = desc->cache_stride_seq;
+    a.cs_tok = desc->cache_stride_token;
+    a.cs_head = desc->cache_stride_head;
+    a.tokens = desc->num_tokens;
+    a.batch = desc->batch;
+    a.hq = desc->num_q_heads;
+    a.hkv = desc->num_kv_heads;
+    a.group = p.group;
+    a.max_kv = desc->max_kv_len;
+    // (A block past the longest cache is the whole cache; sums of it and a position
+    // stay in 32 bits.)
+    a.mask_block = std::min(desc->mask_block, std::max(desc->max_kv_len, 1));
+    a.page_size = std::max(desc->page_size, 1);
+    a.page_shift = (a.page_size & (a.page_size - 1)) == 0 ? __builtin_ctz(a.page_size) : -1;
+    a.max_pages = desc->max_pages_per_seq;
+    a.rows_pb = p.rows_pb;
+    a.blocks = p.blocks;
+    a.chunk = p.chunk;
+    a.scale_log2 = p.scale_log2;
+    const hipError_t e = launch_chunk(*desc, p, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "simsd_chunk_attention launch");
+    return SIMSD_OK;
+  } catch (...) {
+    set_error("simsd_chunk_attention: internal error");
     return SIMSD_ERR_HIP;
   }
 }

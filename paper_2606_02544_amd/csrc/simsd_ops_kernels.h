@@ -29,6 +29,26 @@ struct RotaryArgs {
   float factor;
 };
 
+struct ChunkArgs {
+  const void* q;
+  const void* k_cache;
+  const void* v_cache;
+  const int32_t* block_table;   // null: contiguous
+  const int32_t* q_starts;
+  const int32_t* kv_lens;
+  void* out;
+  float* lse;
+  float* part;                  // split partials (workspace)
+  float2* part_ml;
+  int64_t cs_seq, cs_tok, cs_head;
+  int tokens, batch, hq, hkv, group, mask_block, max_kv, page_size, page_shift, max_pages;
+  int rows_pb, blocks, chunk;
+  float scale_log2;
+};
+
+hipError_t launch_chunk(const simsd_chunk_desc& d, const ChunkPlan& p, const ChunkArgs& a,
+                        hipStream_t stream);
+
 struct SampleArgs {
   const void* logits;
   const float* uniforms;

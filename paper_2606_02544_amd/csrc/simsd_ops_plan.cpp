@@ -146,6 +146,112 @@ simsd_status check_rotary_append_args(const simsd_rotary_desc* d, const void* q,
   return SIMSD_OK;
 }
 
+simsd_status plan_chunk(const simsd_chunk_desc* d, int cus, ChunkPlan* p) {
+  if (!d || !p) return fail(SIMSD_ERR_NULL_POINTER, "chunk_attention: descriptor is NULL");
+  if (cus < 1) return fail(SIMSD_ERR_HIP, "chunk_attention: the device reports no compute units");
+  if (!known_dtype(d->dtype))
+    return fail(SIMSD_ERR_UNSUPPORTED, "chunk_attention: dtype must be SIMSD_F32 or SIMSD_BF16");
+  if (d->num_tokens < 0 || d->num_tokens > (1 << 23))
+    return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: num_tokens must be in [0, 2^23]");
+  if (d->batch < 1 || d->batch > 65535)
+    return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: batch must be in [1, 65535]");
+  if (d->num_q_heads < 1 || d->num_kv_heads < 1 || d->num_q_heads % d->num_kv_heads != 0)
+    return fail(SIMSD_ERR_BAD_SHAPE,
+                "chunk_attention: need num_q_heads, num_kv_heads >= 1 and Hq % Hkv == 0");
+  if (d->num_q_heads / d->num_kv_heads > kMaxGroup)
+    return fail(SIMSD_ERR_UNSUPPORTED, "chunk_attention: Hq / Hkv must be <= 16");
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(SIMSD_ERR_UNSUPPORTED, "chunk_attention: head_dim must be 64 or 128");
+  if (d->max_q_len < 0) return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: max_q_len < 0");
+  if (d->max_kv_len < 0 || d->max_kv_len > (1 << 30))
+    return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: max_kv_len must be in [0, 2^30]");
+  if (d->mask_block < 0) return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: mask_block < 0");
+  if (d->page_size < 0) return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: page_size < 0");
+  if (d->page_size > 0 && d->max_pages_per_seq < ceil_div(d->max_kv_len, d->page_size))
+    return fail(SIMSD_ERR_BAD_SHAPE,
+                "chunk_attention: max_pages_per_seq < ceil(max_kv_len / page_size)");
+  if (d->kv_chunk < 0 || d->kv_chunk % kTile != 0)
+    return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: kv_chunk must be 0 (auto) or a multiple of 64");
+  const int64_t strides[3] = {d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head};
+  const simsd_status st = check_strides("chunk_attention", strides, 3, d->dtype == SIMSD_F32 ? 4 : 2, 48);
+  if (st != SIMSD_OK) return st;
+  if (!(std::isfinite(d->scale) && d->scale >= 0.f))
+    return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: scale must be finite and >= 0");
+
+  ChunkPlan r;
+  r.group = d->num_q_heads / d->num_kv_heads;
+  const int64_t rows = int64_t{std::min(d->max_q_len, d->num_tokens)} * r.group;   // of the longest sequence
+  if (d->dtype == SIMSD_BF16) {
+    // Row waves of 32 rows: two (each paired with a wave for the other half of the
+    // keys, two work-groups a CU), four, or eight (one work-group a CU).
+    r.row_waves = rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+    r.rows_pb = 32 * r.row_waves;
+  } else {
+    r.row_waves = 4;
+    r.rows_pb = rows <= 16 ? 16 : 32;
+  }
+  const int64_t blocks = int64_t{d->num_tokens} * r.group / r.rows_pb + d->batch;
+  if (blocks * d->num_kv_heads > (1 << 22))
+    return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: too many tokens and sequences for one call");
+  r.blocks = static_cast<int>(blocks);
+  // Keys per work-group: all of a row's, unless there are too few row blocks to
+  // fill the chip.
+  const int64_t slots = (r.row_waves >= 4 && d->dtype == SIMSD_BF16 ? 1 : 2) * int64_t{cus};
+  const int64_t groups = blocks * d->num_kv_heads;
+  int64_t most = std::max<int64_t>(ceil_div(d->max_kv_len, kTile) * kTile, kTile);
+  if (d->page_size > 0)   // a work-group holds the ids of its pages in LDS
+    most = std::min(most, std::max<int64_t>(int64_t{kMaxChunkPages - 1} * d->page_size / kTile * kTile, kTile));
+  int64_t chunk = most;
+  if (d->kv_chunk > 0) {
+    chunk = d->kv_chunk;
+  } else if (groups < 4 * slots) {
+    chunk = ceil_div(ceil_div(int64_t{d->max_kv_len} * groups, 4 * slots), kTile) * kTile;
+    chunk = std::max<int64_t>(chunk, 256);
+  }
+  chunk = std::min(chunk, most);
+  r.chunk = static_cast<int>(chunk);
+  r.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(d->max_kv_len, chunk)));
+  if (r.splits > 65535) return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: too many key ranges");
+  if (r.splits > 1 && d->num_tokens > 0) {
+    const size_t n = static_cast<size_t>(r.splits) * d->num_tokens * d->num_q_heads;
+    r.ml_off = n * d->head_dim * sizeof(float);
+    r.workspace = r.ml_off + n * 2 * sizeof(float);
+  }
+  const float scale = d->scale > 0.f ? d->scale : 1.0f / std::sqrt(static_cast<float>(d->head_dim));
+  r.scale_log2 = scale * 1.4426950408889634f;
+  *p = r;
+  return SIMSD_OK;
+}
+
+simsd_status check_chunk_args(const simsd_chunk_desc* d, const ChunkPlan& p, const void* q,
+                              const void* k_cache, const void* v_cache, const int32_t* block_table,
+                              const int32_t* q_starts, const int32_t* kv_lens, const void* out,
+                              const float* lse, const void* workspace, size_t workspace_bytes) {
+  if (d->num_tokens == 0) return SIMSD_OK;
+  if (!q || !q_starts || !kv_lens || !out)
+    return fail(SIMSD_ERR_NULL_POINTER, "chunk_attention: q, q_starts, kv_lens and out are required");
+  if (d->max_kv_len > 0 && (!k_cache || !v_cache))
+    return fail(SIMSD_ERR_NULL_POINTER, "chunk_attention: k_cache/v_cache required when max_kv_len > 0");
+  if (d->page_size > 0 && d->max_kv_len > 0 && !block_table)
+    return fail(SIMSD_ERR_NULL_POINTER, "chunk_attention: block_table required for a paged cache");
+  const void* data[] = {q, k_cache, v_cache, out};
+  for (const void* a : data)
+    if (!aligned(a, 16))
+      return fail(SIMSD_ERR_ALIGNMENT, "chunk_attention: q, the caches and out must be 16-byte aligned");
+  const void* words[] = {block_table, q_starts, kv_lens, lse};
+  for (const void* a : words)
+    if (!aligned(a, 4)) return fail(SIMSD_ERR_ALIGNMENT, "chunk_attention: arrays must be 4-byte aligned");
+  if (p.workspace > 0) {
+    if (!workspace) return fail(SIMSD_ERR_WORKSPACE, "chunk_attention: workspace is NULL");
+    if (!aligned(workspace, 16))
+      return fail(SIMSD_ERR_ALIGNMENT, "chunk_attention: workspace must be 16-byte aligned");
+    if (workspace_bytes < p.workspace)
+      return fail(SIMSD_ERR_WORKSPACE,
+                  "chunk_attention: workspace smaller than simsd_chunk_attention_workspace_size()");
+  }
+  return SIMSD_OK;
+}
+
 simsd_status plan_sample(const simsd_sample_desc* d, double* one) {
   if (!d || !one) return fail(SIMSD_ERR_NULL_POINTER, "sample: descriptor is NULL");
   if (!known_dtype(d->dtype))

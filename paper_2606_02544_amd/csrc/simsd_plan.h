@@ -11,6 +11,7 @@
 namespace simsd {
 
 constexpr int kTile = 64;            // keys per attention tile
+constexpr int kMaxChunkPages = 2048;  // page ids of one key range staged in LDS
 constexpr int kMaxNew = 64;          // B + L limit (one 64-bit visibility word per row)
 constexpr int kMaxGroup = 16;        // Hq / Hkv limit
 constexpr int kStreamChunk = -1;    // kv_chunk value that asks for the stream decomposition
