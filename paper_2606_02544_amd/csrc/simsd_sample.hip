@@ -36,6 +36,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int NT = 512;          // threads of a work-group
 constexpr int NW = NT / 64;
@@ -43,7 +44,7 @@ constexpr int kRegs = 38;        // 16-byte loads of a bf16 row that a lane keep
 constexpr double kCut = 700.0;   // a token further below the maximum, in temperatures, is never kept
 
 struct Params {
-  double T, top_p, min_p;
+  double T, inv, top_p, min_p;   // inv = 1 / T
   uint32_t top_k;                // 0: off
   bool greedy;
 };
@@ -55,9 +56,10 @@ struct Found {
   uint64_t z_before, w;          // weight above it, weight of one such token
 };
 
-__device__ inline uint64_t shfl_up64(uint64_t v, int d) {
-  const uint32_t lo = __shfl_up(static_cast<uint32_t>(v), d), hi = __shfl_up(static_cast<uint32_t>(v >> 32), d);
-  return (static_cast<uint64_t>(hi) << 32) | lo;
+// Value of the lane that the DPP control names, 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t moved(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xf, false));
 }
 __device__ inline uint64_t lane64(uint64_t v, int l) {
   const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), l);
@@ -70,20 +72,27 @@ struct Sum {
   uint64_t z;
 };
 
-__device__ inline Sum wave_scan(Sum v, int lane) {      // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t n = __shfl_up(v.n, d);
-    const uint64_t z = shfl_up64(v.z, d);
-    if (lane >= d) {
-      v.n += n;
-      v.z += z;
-    }
-  }
+template <int CTRL, int ROWS>
+__device__ inline void add_moved(Sum& v) {
+  const uint32_t n = moved<CTRL, ROWS>(v.n);
+  const uint64_t lo = moved<CTRL, ROWS>(static_cast<uint32_t>(v.z));
+  const uint64_t hi = moved<CTRL, ROWS>(static_cast<uint32_t>(v.z >> 32));
+  v.n += n;
+  v.z += hi << 32 | lo;
+}
+// Inclusive sums over the lanes: shifts by 1, 2, 4 and 8 within rows of 16, then
+// the last lanes of rows into the rows after them.
+__device__ inline Sum wave_scan(Sum v) {
+  add_moved<0x111, 0xf>(v);
+  add_moved<0x112, 0xf>(v);
+  add_moved<0x114, 0xf>(v);
+  add_moved<0x118, 0xf>(v);
+  add_moved<0x142, 0xa>(v);
+  add_moved<0x143, 0xc>(v);
   return v;
 }
 
-__device__ inline double weight(double gap, double T) { return exp(gap / T); }
+__device__ inline double weight(double gap, const Params& p) { return exp(gap * p.inv); }
 
 // The row's segments: wave w holds the 16-byte vectors [w*seg, (w+1)*seg) of the
 // row's aligned part, lane by lane; wave 0 also the entries before it (`extra`
@@ -113,32 +122,59 @@ __device__ inline Segment segment_of(const void* row, int V, int wave, int lane)
   return s;
 }
 
-// f(j, vector) for this wave's vectors: from registers, or loaded.  Lanes past the
-// end get the pattern of a NaN, which no filter keeps.
+// Lanes past the end of a row hold the pattern of a NaN, which no filter keeps.
 constexpr uint32_t kNone = 0xffffffffu;
-template <bool REG, typename F>
-__device__ inline __attribute__((always_inline)) void each_vector(const u32x4 (&reg)[kRegs], const Segment& s, int lane, F f) {
-  if constexpr (REG) {
+
+// The wave's vectors in registers (rows of up to NW * 64 * kRegs vectors).
+__device__ inline __attribute__((always_inline)) void load_row(u32x4 (&reg)[kRegs], const Segment& s, int lane) {
 #pragma unroll
-    for (int j = 0; j < kRegs; ++j)
-      if (j * 64 < s.count) f(j, reg[j]);
-  } else {
-    for (int j = 0; j * 64 < s.count; ++j) {
-      u32x4 v = {kNone, kNone, kNone, kNone};
-      if (j * 64 + lane < s.count) v = s.base[s.first + j * 64 + lane];
-      f(j, v);
-    }
+  for (int j = 0; j < kRegs; ++j) {
+    reg[j] = u32x4{kNone, kNone, kNone, kNone};
+    if (j * 64 + lane < s.count) reg[j] = s.base[s.first + j * 64 + lane];
   }
 }
 
-template <bool REG>
-__device__ inline __attribute__((always_inline)) void load_row(u32x4 (&reg)[kRegs], const Segment& s, int lane) {
-  if constexpr (REG) {
+// f(j, vector) of the vectors in registers.  The code of f is there 38 times, so it
+// is short, and what few vectors need is done by visit().  (Eight to a test of the
+// count: a test each takes more scalar registers than there are; and vectors side by
+// side take more vector registers.)
+template <typename F>
+__device__ inline __attribute__((always_inline)) void each_held(const u32x4 (&reg)[kRegs], const Segment& s, F f) {
 #pragma unroll
-    for (int j = 0; j < kRegs; ++j) {
-      reg[j] = u32x4{kNone, kNone, kNone, kNone};
-      if (j * 64 + lane < s.count) reg[j] = s.base[s.first + j * 64 + lane];
+  for (int b = 0; b < kRegs; b += 8)
+    if (b * 64 < s.count) {
+#pragma unroll
+      for (int j = b; j < (b + 8 < kRegs ? b + 8 : kRegs); ++j) {
+        f(j, reg[j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+}
+
+// f(j, vector) of the wave's vectors as they lie in memory, four loads ahead: those
+// of the bits of `hits` (j < 64), or, without HITS, all of them.
+template <bool HITS, typename F>
+__device__ inline __attribute__((always_inline)) void visit(const Segment& s, uint64_t hits, int lane, F f) {
+  constexpr int U = 4;
+  int next = 0;
+  while (HITS ? hits != 0 : next * 64 < s.count) {
+    int j[U];
+    u32x4 v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (HITS) {
+        j[i] = hits ? __builtin_ctzll(hits) : -1;
+        hits &= hits - 1;
+      } else {
+        j[i] = next * 64 < s.count ? next : -1;
+        ++next;
+      }
+      v[i] = u32x4{kNone, kNone, kNone, kNone};
+      if (j[i] >= 0 && j[i] * 64 + lane < s.count) v[i] = s.base[s.first + j[i] * 64 + lane];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (j[i] >= 0) f(j[i], v[i]);
   }
 }
 
@@ -151,6 +187,7 @@ __device__ inline Params params_of(const SampleArgs& a, int r) {
   p.top_p = static_cast<double>(a.top_ps ? a.top_ps[r] : a.top_p);
   p.min_p = static_cast<double>(a.min_ps ? a.min_ps[r] : a.min_p);
   p.greedy = !(p.T > 0.0);
+  p.inv = 1.0 / p.T;
   p.top_k = k > 0 ? k : 0;
   return p;
 }
@@ -162,65 +199,57 @@ __device__ inline uint64_t draw_target(float u, uint64_t z) {
   return t < z ? t : z - 1;
 }
 
-// The index of the rank-th entry (0-based, in vocabulary order) that `match`es,
-// found by the wave that holds it, which writes the outputs.  `count` is this
-// lane's number of matches.
-template <bool BF16, bool REG, typename Match>
+// Inclusive sum of a count over the lanes.
+__device__ inline uint32_t count_scan(uint32_t v) {
+  v += moved<0x111, 0xf>(v);
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);
+  v += moved<0x143, 0xc>(v);
+  return v;
+}
+__device__ inline uint32_t last_lane(uint32_t v) { return __builtin_amdgcn_readlane(v, 63); }
+
+// The index of the rank-th entry (0-based, in vocabulary order) that matches, found
+// by the wave that holds it, which writes the outputs.  `bits`: which entries of a
+// vector match; `hits`: the vectors to look at, as in visit().
+template <int VEC, bool HITS, typename Bits>
 __device__ inline __attribute__((always_inline)) void find_and_write(
-    const SampleArgs& a, int r, const u32x4 (&reg)[kRegs], const Segment& s, uint32_t count,
-    uint32_t rank, float prob, uint32_t kept, int wave, int lane, uint32_t* s_count, bool extra_match, Match match) {
-  constexpr int VEC = BF16 ? 8 : 4;
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) count += __shfl_xor(count, d);
+    const SampleArgs& a, int r, const Segment& s, uint64_t hits, uint32_t rank, float prob, uint32_t kept,
+    int wave, int lane, uint32_t* s_count, bool extra_match, Bits bits) {
+  uint32_t count = extra_match ? 1 : 0;
+  visit<HITS>(s, hits, lane, [&](int, const u32x4& v) __attribute__((always_inline)) { count += __popc(bits(v)); });
+  count = last_lane(count_scan(count));
   if (lane == 0) s_count[wave] = count;
   __syncthreads();
   uint32_t before = 0;
   for (int w = 0; w < wave; ++w) before += s_count[w];
+  before = __builtin_amdgcn_readfirstlane(before);
   if (rank < before || rank >= before + count) return;   // uniform: another wave's
   uint32_t left = rank - before;
   int found = -1;
-  const uint64_t below = (uint64_t{1} << lane) - 1;
-  auto take = [&](bool m, int index) {                   // one entry a lane, in lane order
-    const uint64_t b = __ballot(m);
-    const uint32_t n = __popcll(b);
-    if (left < n && found < 0) {
-      const bool mine = m && static_cast<uint32_t>(__popcll(b & below)) == left;
-      const int l = __builtin_ctzll(__ballot(mine));
-      found = __builtin_amdgcn_readlane(index, l);
-    }
-    left -= n;
-  };
-  if (wave == 0) take(extra_match && s.extra < s.head, s.extra);
-  each_vector<REG>(reg, s, lane, [&](int j, const u32x4& v) __attribute__((always_inline)) {
-    if (found >= 0) return;
-    uint32_t bits = 0;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) bits |= match(v, e) ? 1u << e : 0u;
-    if (!__ballot(bits != 0)) return;
-    uint32_t incl = __popc(bits);
-    const uint32_t own = incl;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(incl, d);
-      if (lane >= d) incl += o;
-    }
-    const uint32_t total = __builtin_amdgcn_readlane(incl, 63);
-    if (left < total) {
-      const uint32_t ex = incl - own;
-      const bool mine = ex <= left && left < incl;
+  // One step: lanes hold `own` matches each, in order; takes the left-th.
+  auto take = [&](uint32_t b, int index) __attribute__((always_inline)) {   // b: matches, from index on
+    const uint32_t own = __popc(b);
+    const uint32_t incl = count_scan(own), total = last_lane(incl);
+    if (found < 0 && left < total) {
+      const bool mine = incl - own <= left && left < incl;
+      uint32_t skip = left - (incl - own);
       int at = 0;
-      uint32_t skip = left - ex, b = bits;
       if (mine) {
         while (skip--) b &= b - 1;
         at = __builtin_ctz(b);
       }
-      const int index = s.head + (s.first + j * 64 + lane) * VEC + at;
-      found = __builtin_amdgcn_readlane(index, __builtin_ctzll(__ballot(mine)));
-    } else {
-      left -= total;
+      found = __builtin_amdgcn_readlane(index + at, __builtin_ctzll(__ballot(mine)));
     }
+    if (found < 0) left -= total;
+  };
+  if (wave == 0) take(extra_match && s.extra < s.head ? 1 : 0, s.extra);
+  visit<HITS>(s, found >= 0 ? 0 : hits, lane, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+    take(bits(v), s.head + (s.first + j * 64 + lane) * VEC);
   });
-  if (found < 0 && wave == NW - 1) take(extra_match && s.extra >= s.head, s.extra);
+  if (wave == NW - 1) take(extra_match && s.extra >= s.head ? 1 : 0, s.extra);
   if (lane == 0) {
     a.token[r] = found;
     if (a.prob) a.prob[r] = prob;
@@ -238,7 +267,7 @@ __device__ inline void write_none(const SampleArgs& a, int r) {
 
 // Sum over the work-group up to and including each thread; *total for all.
 __device__ inline Sum block_scan(Sum v, int wave, int lane, Sum* s_wave, Sum* total) {
-  v = wave_scan(v, lane);
+  v = wave_scan(v);
   if (lane == 63) s_wave[wave] = v;
   __syncthreads();
   Sum all = {0, 0}, before = {0, 0};
@@ -303,24 +332,311 @@ __device__ inline __attribute__((always_inline)) Found cut_and_draw(const Params
 }
 
 // ----------------------------------------------------------------------------
+// The short way: where few tokens can be kept, they are sorted.
+//
+// A row's candidates are the entries not below a bound that no kept token is
+// under: the maximum itself (T <= 0); the maximum less kCut T; m + T ln(min_p) where
+// top_p is off; and the k-th largest of the maxima of the row's parts (k parts
+// hold an entry not below it; a part is an eighth of a bf16 lane's entries, a quarter
+// of an fp32 lane's).  Up to kCap of them are put in LDS in the order of falling
+// logits and rising index, and every search is one in running sums over that list.
+// ----------------------------------------------------------------------------
+constexpr int kCap = 4096;
+
+struct Small {                   // LDS beside the large arrays
+  Sum wave[NW];
+  uint32_t count[NW];
+  float top[NW];
+  uint32_t tally[2][NW][4];
+  uint32_t listed;
+  Found found;
+};
+struct List {
+  uint64_t key[kCap];            // falling pattern << 32 | index
+  uint64_t sorted[NT];
+};
+
+// Bit patterns of fp32 in rising order; -0 as +0.
+__device__ inline uint32_t ordered(uint32_t b) {
+  if (b == 0x80000000u) b = 0;
+  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+}
+__device__ inline float ordered_float(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+// Entry e of a vector, as fp32 bits.
+template <bool BF16>
+__device__ inline uint32_t entry(const u32x4& v, int e) {
+  if constexpr (BF16) return e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16;
+  else return v[e];
+}
+
+// The largest of the lane's maxima over the work-group.
+__device__ inline float block_maximum(float m, int wave, int lane, Small& sm) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  if (lane == 0) sm.top[wave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) m = fmaxf(m, sm.top[w]);
+  return m;
+}
+
+// Maxima of this lane's parts of the row: key[i] the upper 16 bits of ordered(),
+// and the row's largest entry (-inf if it has none that is a number).
+constexpr uint32_t kNoKey = 0x7f;                // of -inf
+template <bool BF16>
+__device__ inline __attribute__((always_inline)) float part_maxima_read(const Segment& s, uint32_t xbits, int wave, int lane, Small& sm,
+                                                                       uint32_t (&key)[4]) {
+  constexpr int VEC = BF16 ? 8 : 4;
+  float part[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[i] = -__builtin_huge_valf();
+  part[0] = fmaxf(part[0], __uint_as_float(xbits));
+  visit<false>(s, 0, lane, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+    float m = -__builtin_huge_valf();
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) m = fmaxf(m, __uint_as_float(entry<BF16>(v, e)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[i] = (j & 3) == i ? fmaxf(part[i], m) : part[i];
+  });
+#pragma unroll
+  for (int i = 0; i < 4; ++i) key[i] = ordered(__float_as_uint(part[i])) >> 16;
+  return block_maximum(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])), wave, lane, sm);
+}
+// bf16 in registers: two entries at a time as 16-bit integers in the order of their
+// values; NaN of positive sign would be the largest, and sends the row to the other
+// form (*odd).
+__device__ inline __attribute__((always_inline)) float part_maxima_held(const u32x4 (&reg)[kRegs], const Segment& s, uint32_t xbits,
+                                                                       int wave, int lane, Small& sm, uint32_t (&key)[8], bool* odd) {
+  s16x2 part[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[i] = s16x2{-0x8000, -0x8000};
+  auto rising = [](uint32_t w) {
+    const s16x2 x = __builtin_bit_cast(s16x2, w);
+    return x ^ ((x >> s16x2{15, 15}) & s16x2{0x7fff, 0x7fff});
+  };
+  part[0] = __builtin_elementwise_max(part[0], rising(xbits >> 16 | xbits));   // (either half: the entry itself, or 0xffff)
+  each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) part[j % 4] = __builtin_elementwise_max(part[j % 4], rising(v[q]));
+  });
+  int best = -0x8000;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int x = part[i / 2][i % 2];
+    best = max(best, x);
+    key[i] = static_cast<uint32_t>(x + 0x8000);
+  }
+  // Back to the pattern: non-negative ones are themselves.
+  const uint32_t bits = static_cast<uint32_t>(best >= 0 ? best : best ^ 0x7fff) << 16;
+  *odd = __syncthreads_or(best > 0x7f80) != 0;
+  const float m = __uint_as_float(bits);
+  return block_maximum(m == m ? m : -__builtin_huge_valf(), wave, lane, sm);   // (nothing but NaN: -inf)
+}
+
+// A bound that the k-th largest of the parts' maxima is not below, k <= N * NT: its
+// upper 16 bits, two at a time.
+template <int N>
+__device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t k, int wave, int lane, Small& sm) {
+  uint32_t lo = 0;
+  for (int round = 0; round < 8; ++round) {
+    const uint32_t step = 1u << (14 - 2 * round);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) n += __popcll(__ballot(key[i] >= lo + (q + 1) * step));
+      if (lane == 0) sm.tally[round & 1][wave][q] = n;
+    }
+    __syncthreads();                             // (the other buffer's readers are past it, too)
+    uint32_t n[3] = {0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+      for (int q = 0; q < 3; ++q) n[q] += sm.tally[round & 1][w][q];
+    lo += (n[0] >= k ? step : 0) + (n[1] >= k ? step : 0) + (n[2] >= k ? step : 0);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  return lo <= kNoKey ? -__FLT_MAX__ : ordered_float(lo << 16);
+}
+
+// Draws the row's token from the sorted list and writes it; false if there are too
+// many candidates (nothing is written then).  N: parts of a lane.
+template <bool BF16, bool REG, int N>
+__device__ inline __attribute__((always_inline)) bool sample_short(
+    const SampleArgs& a, int r, const u32x4 (&reg)[REG ? kRegs : 1], const Segment& s, uint32_t xbits, const Params& p,
+    float u, float top, const uint32_t (&key)[N], int wave, int lane, Small& sm, List& list) {
+  constexpr int VEC = BF16 ? 8 : 4;
+  const int tid = threadIdx.x;
+  const double m = static_cast<double>(top);
+  // The bound, a little lower than it is (weights and cuts are looked at exactly
+  // later on).
+  auto below = [](double x) { return static_cast<float>(x - fabs(x) * 1e-6); };
+  const bool by_min = p.min_p > 0.0 && !(p.top_p < 1.0);
+  const bool by_k = p.top_k && p.top_k <= N * NT && p.top_k <= kCap / 2;
+  if (!(p.greedy || by_min || by_k || a.V <= kCap || p.T < 0.05)) return false;
+  float bound = top;
+  if (!p.greedy && top < __builtin_huge_valf()) {
+    bound = fmaxf(below(m - kCut * p.T), -__FLT_MAX__);
+    if (by_min) bound = fmaxf(bound, below(m + p.T * log(fmin(p.min_p, 1.0)) - 1e-6 * p.T));
+    if (by_k) bound = fmaxf(bound, kth_bound(key, p.top_k, wave, lane, sm));
+    bound = fminf(bound, top);
+  }
+  if (tid == 0) sm.listed = 0;
+  __syncthreads();
+  auto takes = [&](uint32_t bits) { return __uint_as_float(bits) >= bound; };   // (false for NaN)
+  // `b`: which of a lane's entries from `index` on are candidates.
+  auto list_them = [&](uint32_t b, int index, auto bits_of) __attribute__((always_inline)) {
+    const uint32_t own = __popc(b), incl = count_scan(own), total = last_lane(incl);
+    if (total == 0) return;
+    uint32_t at = 0;
+    if (lane == 0) at = atomicAdd(&sm.listed, total);
+    at = __builtin_amdgcn_readfirstlane(at) + incl - own;
+    for (; b; b &= b - 1) {
+      const int e = __builtin_ctz(b);
+      if (at < kCap) list.key[at] = static_cast<uint64_t>(~ordered(bits_of(e))) << 32 | static_cast<uint32_t>(index + e);
+      ++at;
+    }
+  };
+  uint64_t hits = 0;                             // vectors with a candidate in the wave
+  if constexpr (REG)
+    each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+      bool t = false;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) t = t | takes(entry<BF16>(v, e));
+      if (__ballot(t)) hits |= uint64_t{1} << j;
+    });
+  list_them(takes(xbits) ? 1 : 0, s.extra, [&](int) { return xbits; });
+  visit<REG>(s, hits, lane, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) b |= takes(entry<BF16>(v, e)) ? 1u << e : 0u;
+    list_them(b, s.head + (s.first + j * 64 + lane) * VEC, [&](int e) {
+      const uint32_t w = v[BF16 ? e / 2 : e];
+      return BF16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w;
+    });
+  });
+  __syncthreads();
+  const int n = static_cast<int>(__builtin_amdgcn_readfirstlane(sm.listed));
+  if (n > kCap) return false;
+
+  // In order: by rank where each thread has one candidate, else in pairs.
+  const uint64_t* sorted = list.key;
+  if (n <= NT) {
+    const uint64_t mine = tid < n ? list.key[tid] : 0;
+    int rank = 0;
+    for (int i = 0; i < n; ++i) rank += list.key[i] < mine ? 1 : 0;
+    if (tid < n) list.sorted[rank] = mine;
+    sorted = list.sorted;
+    __syncthreads();
+  } else {
+    int size = 2 * NT;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += NT) list.key[i] = ~uint64_t{0};
+    for (int k = 2; k <= size; k *= 2)
+      for (int d = k / 2; d >= 1; d /= 2) {
+        __syncthreads();
+        for (int t = tid; t < size / 2; t += NT) {
+          const int i = (t & ~(d - 1)) * 2 + (t & (d - 1)), j = i + d;
+          const uint64_t x = list.key[i], y = list.key[j];
+          if ((x > y) == ((i & k) == 0)) {
+            list.key[i] = y;
+            list.key[j] = x;
+          }
+        }
+      }
+    __syncthreads();
+  }
+
+  if (p.greedy) {
+    if (tid == 0) {
+      a.token[r] = static_cast<int32_t>(sorted[0]);
+      if (a.prob) a.prob[r] = 1.f;
+      if (a.kept) a.kept[r] = 1;
+    }
+    return true;
+  }
+  // Thread t holds the candidates from t * per on.
+  const int per = (n + NT - 1) / NT, first = tid * per;
+  auto gap_at = [&](int i) {
+    const float x = ordered_float(~static_cast<uint32_t>(sorted[i] >> 32));
+    return x == top ? 0.0 : static_cast<double>(x) - m;
+  };
+  auto fixed_at = [&](int i, double* w) {        // 0 past the end and for what is never kept
+    *w = -1.0;
+    if (i >= n) return uint64_t{0};
+    const double gap = gap_at(i);
+    if (!(gap >= -kCut * p.T)) return uint64_t{0};
+    *w = weight(gap, p);
+    return static_cast<uint64_t>(rint(*w * a.one));
+  };
+  Sum mine = {0, 0}, by_min_mine = {0, 0}, all;
+  for (int e = 0; e < per; ++e) {
+    double w;
+    const uint64_t z = fixed_at(first + e, &w);
+    if (w >= 0.0) mine = Sum{mine.n + 1, mine.z + z};
+    if (w >= fmin(p.min_p, 1.0)) by_min_mine = Sum{by_min_mine.n + 1, by_min_mine.z + z};
+  }
+  const Sum incl = block_scan(mine, wave, lane, sm.wave, &all);
+  const Sum excl = {incl.n - mine.n, incl.z - mine.z};
+  Sum by_min_all = all;
+  if (p.min_p > 0.0) block_scan(by_min_mine, wave, lane, sm.wave, &by_min_all);
+  auto find = [&](Kind kind, uint64_t target) __attribute__((always_inline)) {
+    if (reached(kind, incl, target) && !reached(kind, excl, target)) {
+      Sum before = excl;
+      for (int e = 0; e < per; ++e) {
+        double w;
+        const uint64_t z = fixed_at(first + e, &w);
+        const Sum next = {before.n + 1, before.z + z};
+        if (reached(kind, next, target)) {
+          sm.found = Found{static_cast<uint32_t>(first + e), before.n, 1, before.z, z};
+          break;
+        }
+        before = next;
+      }
+    }
+    __syncthreads();
+    const Found f = sm.found;
+    __syncthreads();
+    return f;
+  };
+  uint32_t rank;
+  Sum kept;
+  const Found f = cut_and_draw(p, all, by_min_all, u, &rank, &kept, find);
+  if (tid == 0) {
+    a.token[r] = static_cast<int32_t>(sorted[f.key]);
+    if (a.prob) a.prob[r] = static_cast<float>(weight(gap_at(f.key), p) * a.one / static_cast<double>(kept.z));
+    if (a.kept) a.kept[r] = static_cast<int32_t>(kept.n);
+  }
+  return true;
+}
+
+// ----------------------------------------------------------------------------
 // bf16
 // ----------------------------------------------------------------------------
 // Place of a bit pattern in the falling order: positive ones from the largest
 // (+0 last), then negative ones from -0 on.  -0 counts as +0.
 constexpr uint32_t kInfPlace = 0x7f, kZeroPlace = 0x7fff, kEndPlace = 0xff80;   // +inf; +0; -inf
 __device__ inline uint32_t place_bits(uint32_t o) { return o < 0x8000u ? 0x7fffu - o : o; }
+__device__ inline uint32_t place_of(uint32_t bits) { return bits < 0x8000u ? 0x7fffu - bits : bits; }
 __device__ inline double place_value(uint32_t o) { return static_cast<double>(__uint_as_float(place_bits(o) << 16)); }
 
 constexpr int kSteps = 512;      // 128 places each
 constexpr int kWraps = 256;      // notes of wraps at most: 2^22 entries wrap 64 counters, with up to 3 notes each
 
 struct Bf16Shared {
-  uint32_t hist[32768];          // counts of patterns 2i (low half) and 2i + 1 (high half)
+  union {
+    uint32_t hist[32768];        // counts of patterns 2i (low half) and 2i + 1 (high half)
+    List list;
+  };
   uint32_t n[kSteps];            // tokens of the steps above (exclusive), after the scan
   uint64_t z[kSteps];
-  Sum wave[NW];
-  uint32_t count[NW];
-  uint32_t top, total, wraps, step;
+  Small small;
+  uint64_t live[NW];             // steps with any count
+  uint32_t total, wraps, step;
+  uint8_t any[kSteps];
   int32_t wrap[kWraps];          // pattern whose count grew by 65536, or ~pattern: by one too many
 };
 
@@ -332,12 +648,43 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const void* row = static_cast<const uint16_t*>(a.logits) + static_cast<int64_t>(r) * a.V;
   const Segment s = segment_of<true>(row, a.V, wave, lane);
-  u32x4 reg[kRegs];
-  load_row<REG>(reg, s, lane);
-  uint32_t xbits = kNone;                        // this lane's entry outside the vectors
-  if (s.extra >= 0) xbits = static_cast<const uint16_t*>(row)[s.extra];
+  u32x4 reg[REG ? kRegs : 1];
+  if constexpr (REG) load_row(reg, s, lane);
+  uint32_t xbits = kNone;                        // this lane's entry outside the vectors, as fp32
+  if (s.extra >= 0) xbits = static_cast<uint32_t>(static_cast<const uint16_t*>(row)[s.extra]) << 16;
   const Params p = params_of(a, r);
   const float u = a.uniforms[r];
+  float best;
+  if constexpr (REG) {
+    uint32_t key[8];
+    bool odd;
+    best = part_maxima_held(reg, s, xbits, wave, lane, sh.small, key, &odd);
+    if (odd) {
+      uint32_t key4[4];
+      __syncthreads();                           // the first maxima are read
+      best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) key[i] = i < 4 ? key4[i] : kNoKey;
+    }
+    if (best > -__builtin_huge_valf() &&
+        sample_short<true, true>(a, r, reg, s, xbits, p, u, best, key, wave, lane, sh.small, sh.list))
+      return;
+  } else {
+    uint32_t key[4];
+    best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key);
+    if (best > -__builtin_huge_valf() &&
+        sample_short<true, false>(a, r, reg, s, xbits, p, u, best, key, wave, lane, sh.small, sh.list))
+      return;
+  }
+  if (best == -__builtin_huge_valf()) {
+    write_none(a, r);
+    return;
+  }
+  __syncthreads();                               // the list's LDS becomes the histogram's
+  // The largest entry's place (-0 is +0).
+  const uint32_t top = best == 0.f ? kZeroPlace : place_of(__float_as_uint(best) >> 16);
+  const double m = place_value(top);
+  const double scale = a.one;
 
   // One count of a pattern; NOTE: a counter that wraps is noted.
   auto add = [&](uint32_t twice, uint32_t one, auto note) __attribute__((always_inline)) {
@@ -363,34 +710,45 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
     u32x4* h = reinterpret_cast<u32x4*>(sh.hist);
     for (int i = tid; i < 32768 / 4; i += NT) h[i] = u32x4{0, 0, 0, 0};
     if (tid == 0) {
-      sh.top = kEndPlace;
       sh.total = 0;
       sh.wraps = 0;
     }
     __syncthreads();
-    each_vector<REG>(reg, s, lane, [&](int j, const u32x4& v) __attribute__((always_inline)) {
-      if (j * 64 + lane < s.count) {
+    auto add_all = [&](int, const u32x4& v) __attribute__((always_inline)) {
+      if ((v[0] & v[1] & v[2] & v[3]) != kNone) {   // (all NaN, or past the end)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           add((v[q] << 1) & 0x1fffcu, 1u << ((v[q] << 4) & 16u), note);
           add((v[q] >> 15) & 0x1fffcu, 1u << ((v[q] >> 12) & 16u), note);
         }
       }
-    });
-    if (s.extra >= 0) add((xbits << 1) & 0x1fffcu, 1u << ((xbits << 4) & 16u), note);
+    };
+    if constexpr (REG && !decltype(note)::value) each_held(reg, s, add_all);
+    else visit<false>(s, 0, lane, add_all);
+    if (s.extra >= 0) add((xbits >> 15) & 0x1fffcu, 1u << ((xbits >> 12) & 16u), note);
     __syncthreads();
-    // The sum of all counts.  (-inf and the odd pattern beside it, a NaN, are
-    // never kept: their word counts as one number, so masking with -inf wraps
-    // nothing.)
+    // The sum of all counts, and which steps have any (a wave reads the words of
+    // one step at a time).  (-inf and the odd pattern beside it, a NaN, are never
+    // kept: their word counts as one number, so masking with -inf wraps nothing.)
     uint32_t sum = 0;
-    for (int i = tid; i < 32768; i += NT) {
-      const uint32_t w = sh.hist[i];
-      sum += i == kEndPlace / 2 ? w : (w & 0xffffu) + (w >> 16);
+#pragma unroll 8
+    for (int i = 0; i < 32768 / NT; ++i) {
+      const int at = i * NT + tid;
+      const uint32_t w = sh.hist[at];
+      sum += at == kEndPlace / 2 ? w : (w & 0xffffu) + (w >> 16);
+      const int group = i * NW + wave;
+      const bool live = __ballot(w != 0) != 0;
+      if (lane == 0) sh.any[group < kSteps / 2 ? kSteps / 2 - 1 - group : group] = live;
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
     if (lane == 0) atomicAdd(&sh.total, sum);
     __syncthreads();
+    if constexpr (decltype(note)::value) {       // counts of 65536 read 0
+      for (uint32_t i = tid; i < sh.wraps; i += NT)
+        if (sh.wrap[i] >= 0) sh.any[place_of(sh.wrap[i]) / 128] = 1;
+      __syncthreads();
+    }
   };
   build(std::false_type{});
   if (sh.total != static_cast<uint32_t>(a.V)) {
@@ -422,25 +780,6 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
     if (o + 1 < kInfPlace) c[1] = 0;
     if (o >= kEndPlace) c[0] = c[1] = 0;
   };
-  uint32_t top = kEndPlace;                      // the row's largest entry
-  for (uint32_t step = wave; step < kSteps && top == kEndPlace; step += NW) {
-    uint32_t c[2];
-    counts(step, c);
-    const uint64_t b0 = __ballot(c[0] != 0), b1 = __ballot(c[1] != 0);
-    if (b0 | b1) {
-      const int l = __builtin_ctzll(b0 | b1);
-      top = step * 128 + 2 * l + ((b0 >> l) & 1 ? 0 : 1);
-    }
-  }
-  if (lane == 0) atomicMin(&sh.top, top);
-  __syncthreads();
-  top = __builtin_amdgcn_readfirstlane(sh.top);
-  if (top == kEndPlace) {
-    write_none(a, r);
-    return;
-  }
-  const double m = place_value(top);
-  const double scale = a.one;
   // Count and weight of one place (0, 0 where it is too far below the top).
   auto place_sum = [&](uint32_t o, uint32_t c, uint64_t* w) __attribute__((always_inline)) {
     Sum v = {0, 0};
@@ -448,7 +787,7 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
     if (c) {
       const double gap = o == top ? 0.0 : place_value(o) - m;
       if (gap >= -kCut * p.T) {
-        *w = static_cast<uint64_t>(rint(weight(gap, p.T) * scale));
+        *w = static_cast<uint64_t>(rint(weight(gap, p) * scale));
         v.n = c;
         v.z = c * *w;
       }
@@ -459,30 +798,40 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
   uint32_t place = top, rank = 0, kept = 1;
   float prob = 1.f;
   if (!p.greedy) {
-    // Sums of the steps, dealt to the waves in turn (a row's values lie close
-    // together in the order).
-    for (uint32_t step = wave; step < kSteps; step += NW) {
-      uint32_t c[2];
-      counts(step, c);
-      Sum v = {0, 0};
-      if (__ballot((c[0] | c[1]) != 0)) {
+    // Sums of the steps that have any count, dealt to the waves in turn (a row's
+    // values lie close together in the order).
+    sh.n[tid] = 0;
+    sh.z[tid] = 0;
+    const uint64_t live = __ballot(sh.any[tid] != 0);
+    if (lane == 0) sh.live[wave] = live;
+    __syncthreads();
+    int turn = 0;
+    for (int q = 0; q < NW; ++q) {
+      uint64_t left = sh.live[q];
+      left = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(left >> 32))) << 32 |
+             static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(left)));
+      for (; left; left &= left - 1) {
+        if ((turn++ & (NW - 1)) != wave) continue;
+        const uint32_t step = q * 64 + __builtin_ctzll(left);
+        uint32_t c[2];
+        counts(step, c);
         uint64_t w;
-        v = place_sum(step * 128 + 2 * lane, c[0], &w);
+        Sum v = place_sum(step * 128 + 2 * lane, c[0], &w);
         const Sum v1 = place_sum(step * 128 + 2 * lane + 1, c[1], &w);
         v.n += v1.n;
         v.z += v1.z;
-        v = wave_scan(v, lane);
-      }
-      if (lane == 63) {
-        sh.n[step] = v.n;
-        sh.z[step] = v.z;
+        v = wave_scan(v);
+        if (lane == 63) {
+          sh.n[step] = v.n;
+          sh.z[step] = v.z;
+        }
       }
     }
     __syncthreads();
     Sum mine = {0, 0}, all;
     mine = Sum{sh.n[tid], sh.z[tid]};
     static_assert(kSteps == NT, "one step a thread");
-    const Sum incl = block_scan(mine, wave, lane, sh.wave, &all);
+    const Sum incl = block_scan(mine, wave, lane, sh.small.wave, &all);
     const Sum excl = {incl.n - mine.n, incl.z - mine.z};
     sh.n[tid] = excl.n;
     sh.z[tid] = excl.z;
@@ -494,7 +843,7 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
       v[0] = place_sum(step * 128 + 2 * lane, c[0], &w[0]);
       v[1] = place_sum(step * 128 + 2 * lane + 1, c[1], &w[1]);
       const Sum own = {v[0].n + v[1].n, v[0].z + v[1].z};
-      Sum sc = wave_scan(own, lane);
+      Sum sc = wave_scan(own);
       c[0] = v[0].n;
       c[1] = v[1].n;
       v[0] = Sum{sh.n[step] + sc.n - own.n, sh.z[step] + sc.z - own.z};   // before the first
@@ -527,7 +876,7 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
       for (int shift = 10; shift >= 0; shift -= 5) {
         const uint32_t o = min(lo + (static_cast<uint32_t>(lane) << shift), kEndPlace - 1);
         const double gap = o == top ? 0.0 : place_value(o) - m;
-        const uint64_t b = __ballot(weight(gap, p.T) >= fmin(p.min_p, 1.0));
+        const uint64_t b = __ballot(weight(gap, p) >= fmin(p.min_p, 1.0));
         lo = __builtin_amdgcn_readlane(o, 63 - __builtin_clzll(b));
       }
       Sum v[2];
@@ -544,52 +893,52 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
     place = f.key;
     kept = part.n;
     const double gap = place == top ? 0.0 : place_value(place) - m;
-    prob = static_cast<float>(weight(gap, p.T) * scale / static_cast<double>(part.z));
+    prob = static_cast<float>(weight(gap, p) * scale / static_cast<double>(part.z));
   }
 
   // The rank-th entry with the drawn value, in vocabulary order.
   const uint32_t bits = place_bits(place), two = bits | bits << 16;
   const uint32_t mask = bits == 0 ? 0x7fff7fffu : 0xffffffffu;
-  u16x2 other = {0, 0};                          // entries of this lane that differ
-  uint32_t held = 0;
-  each_vector<REG>(reg, s, lane, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+  uint64_t hits = 0;                             // vectors that hold it
+  if constexpr (REG)
+    each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+      u16x2 x = {1, 1};                          // 0 in a half where an entry is equal
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      other += __builtin_elementwise_min(__builtin_bit_cast(u16x2, (v[q] ^ two) & mask), u16x2{1, 1});
-    held += 8;
-  });
-  const bool extra_match = s.extra >= 0 && ((xbits ^ bits) & mask & 0xffffu) == 0;
-  const uint32_t count = held - other[0] - other[1] + (extra_match ? 1 : 0);
-  find_and_write<true, REG>(a, r, reg, s, count, rank, prob, kept, wave, lane, sh.count, extra_match,
-                            [&](const u32x4& v, int e) __attribute__((always_inline)) {
-                              return (((e & 1 ? v[e / 2] >> 16 : v[e / 2]) ^ bits) & mask & 0xffffu) == 0;
-                            });
+      for (int q = 0; q < 4; ++q) x = __builtin_elementwise_min(x, __builtin_bit_cast(u16x2, (v[q] ^ two) & mask));
+      if (__ballot(x[0] == 0 || x[1] == 0)) hits |= uint64_t{1} << j;
+    });
+  auto equal = [&](const u32x4& v) __attribute__((always_inline)) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t x = (v[q] ^ two) & mask;
+      b |= ((x & 0xffffu) == 0 ? 1u : 0u) << 2 * q | ((x >> 16) == 0 ? 2u : 0u) << 2 * q;
+    }
+    return b;
+  };
+  const bool extra_match = s.extra >= 0 && ((xbits >> 16 ^ bits) & mask & 0xffffu) == 0;
+  find_and_write<8, REG>(a, r, s, hits, rank, prob, kept, wave, lane, sh.small.count, extra_match, equal);
 }
 
 // ----------------------------------------------------------------------------
 // fp32
 // ----------------------------------------------------------------------------
-// Bit patterns in rising order; -0 as +0.
-__device__ inline uint32_t ordered(uint32_t b) {
-  if (b == 0x80000000u) b = 0;
-  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
-}
-__device__ inline double ordered_value(uint32_t k) {
-  return static_cast<double>(__uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k));
-}
+__device__ inline double ordered_value(uint32_t k) { return static_cast<double>(ordered_float(k)); }
 
 constexpr int kBins = 8192, kMid = 1024;   // upper 13 bits; next 10 (and the last 9)
 static_assert(kMid == 2 * NT, "two or one bins of the lower levels a thread");
 
 struct F32Shared {
-  uint64_t z[kBins];
-  uint32_t n[kBins];
-  uint64_t z2[kMid];
-  uint32_t n2[kMid];
-  Sum wave[NW];
-  uint32_t count[NW];
-  float top[NW];
-  Found found;
+  union {
+    struct {
+      uint64_t z[kBins];
+      uint32_t n[kBins];
+      uint64_t z2[kMid];
+      uint32_t n2[kMid];
+    };
+    List list;
+  };
+  Small small;
 };
 
 __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
@@ -603,41 +952,31 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
   if (s.extra >= 0) xbits = static_cast<const uint32_t*>(row)[s.extra];
   const Params p = params_of(a, r);
   const float u = a.uniforms[r];
-  for (int i = tid; i < kBins; i += NT) {
-    sh.z[i] = 0;
-    sh.n[i] = 0;
-  }
-
-  auto each = [&](auto f) __attribute__((always_inline)) {   // f(bits) of every entry (NaN past the end)
-    constexpr int U = 4;                         // loads ahead
-    for (int j = 0; j < s.count; j += 64 * U) {
-      u32x4 v[U];
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        v[i] = u32x4{kNone, kNone, kNone, kNone};
-        if (j + 64 * i + lane < s.count) v[i] = s.base[s.first + j + 64 * i + lane];
-      }
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          f(v[i][q]);
-          __builtin_amdgcn_sched_barrier(0);   // (sixteen exps side by side take more registers than there are)
-        }
-    }
-    f(xbits);
-  };
-  float best = -__builtin_huge_valf();
-  each([&](uint32_t b) __attribute__((always_inline)) { best = fmaxf(best, __uint_as_float(b)); });
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) best = fmaxf(best, __shfl_xor(best, d));
-  if (lane == 0) sh.top[wave] = best;
-  __syncthreads();
-  for (int w = 0; w < NW; ++w) best = fmaxf(best, sh.top[w]);
+  const u32x4 none[1] = {};                      // (the row is not kept in registers)
+  uint32_t part[4];
+  const float best = part_maxima_read<false>(s, xbits, wave, lane, sh.small, part);
   if (best == -__builtin_huge_valf()) {
     write_none(a, r);
     return;
   }
+  if (sample_short<false, false>(a, r, none, s, xbits, p, u, best, part, wave, lane, sh.small, sh.list)) return;
+  __syncthreads();                               // the list's LDS becomes the bins'
+  for (int i = tid; i < kBins; i += NT) {
+    sh.z[i] = 0;
+    sh.n[i] = 0;
+  }
+  __syncthreads();
+
+  auto each = [&](auto f) __attribute__((always_inline)) {   // f(bits) of every entry (NaN past the end)
+    visit<false>(s, 0, lane, [&](int, const u32x4& v) __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f(v[q]);
+        __builtin_amdgcn_sched_barrier(0);       // (exps side by side take more registers than there are)
+      }
+    });
+    f(xbits);
+  };
   const double m = static_cast<double>(best), scale = a.one;
   const uint32_t top = ordered(__float_as_uint(best));
 
@@ -645,7 +984,7 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
   auto gap_of = [&](uint32_t b) __attribute__((always_inline)) {
     return __uint_as_float(b) == best ? 0.0 : static_cast<double>(__uint_as_float(b)) - m;
   };
-  auto fixed = [&](double gap) { return static_cast<uint64_t>(rint(weight(gap, p.T) * scale)); };
+  auto fixed = [&](double gap) { return static_cast<uint64_t>(rint(weight(gap, p) * scale)); };
   const double least_gap = -kCut * p.T;
 
   uint32_t key = top, rank = 0, kept = 1;
@@ -668,7 +1007,7 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
       mine.n += sh.n[kBins - 1 - tid * PER - i];
       mine.z += sh.z[kBins - 1 - tid * PER - i];
     }
-    const Sum incl = block_scan(mine, wave, lane, sh.wave, &all);
+    const Sum incl = block_scan(mine, wave, lane, sh.small.wave, &all);
     const Sum excl = {incl.n - mine.n, incl.z - mine.z};
 
     // The pattern at which the running sums reach the target: its bin (the
@@ -680,14 +1019,14 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
           const int bin = kBins - 1 - tid * PER - i;
           const Sum next = {at.n + sh.n[bin], at.z + sh.z[bin]};
           if (reached(kind, next, target)) {
-            sh.found = Found{static_cast<uint32_t>(bin), at.n, 0, at.z, 0};
+            sh.small.found = Found{static_cast<uint32_t>(bin), at.n, 0, at.z, 0};
             break;
           }
           at = next;
         }
       }
       __syncthreads();
-      Found f = sh.found;
+      Found f = sh.small.found;
       for (int level = 0; level < 2; ++level) {
         const int bits = level ? 9 : 10, shift = level ? 0 : 9, width = 1 << bits;
         for (int i = tid; i < kMid; i += NT) {
@@ -712,17 +1051,17 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
         const int per = width / NT;
         for (int i = 0; i < 2; ++i)
           if (i < per) v[i] = Sum{sh.n2[width - 1 - tid * per - i], sh.z2[width - 1 - tid * per - i]};
-        Sum in = block_scan(Sum{v[0].n + v[1].n, v[0].z + v[1].z}, wave, lane, sh.wave, &t);
+        Sum in = block_scan(Sum{v[0].n + v[1].n, v[0].z + v[1].z}, wave, lane, sh.small.wave, &t);
         in.n += f.n_before;
         in.z += f.z_before;
         const Sum mid = {in.n - v[1].n, in.z - v[1].z}, ex = {mid.n - v[0].n, mid.z - v[0].z};
         if (reached(kind, in, target) && !reached(kind, ex, target)) {
           const int i = reached(kind, mid, target) ? 0 : 1;
           const Sum before = i ? mid : ex;
-          sh.found = Found{f.key << bits | static_cast<uint32_t>(width - 1 - tid * per - i), before.n, v[i].n, before.z, v[i].z};
+          sh.small.found = Found{f.key << bits | static_cast<uint32_t>(width - 1 - tid * per - i), before.n, v[i].n, before.z, v[i].z};
         }
         __syncthreads();
-        f = sh.found;
+        f = sh.small.found;
       }
       __syncthreads();
       f.w = f.w / f.n;                           // equal patterns weigh the same
@@ -737,7 +1076,7 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
         const uint32_t d = static_cast<uint32_t>(lane) << shift;
         const uint32_t k = hi > d ? hi - d : 0u;
         const double gap = k == top ? 0.0 : ordered_value(k) - m;
-        const uint64_t b = __ballot(weight(gap, p.T) >= least);   // (a NaN's pattern: false)
+        const uint64_t b = __ballot(weight(gap, p) >= least);   // (a NaN's pattern: false)
         hi = __builtin_amdgcn_readlane(k, 63 - __builtin_clzll(b));
       }
       // What the bins above its own hold, and its bin's share.
@@ -761,22 +1100,24 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
           v.z += sh.z[q];
         }
       }
-      block_scan(v, wave, lane, sh.wave, &by_min);
+      block_scan(v, wave, lane, sh.small.wave, &by_min);
     }
     Sum part;
     const Found f = cut_and_draw(p, all, by_min, u, &rank, &part, find);
     key = f.key;
     kept = part.n;
     const double gap = key == top ? 0.0 : ordered_value(key) - m;
-    prob = static_cast<float>(weight(gap, p.T) * scale / static_cast<double>(part.z));
+    prob = static_cast<float>(weight(gap, p) * scale / static_cast<double>(part.z));
   }
 
-  const u32x4 none[kRegs] = {};
-  uint32_t count = 0;
-  each([&](uint32_t b) __attribute__((always_inline)) { count += ordered(b) == key ? 1 : 0; });
   const bool extra_match = s.extra >= 0 && ordered(xbits) == key;
-  find_and_write<false, false>(a, r, none, s, count, rank, prob, kept, wave, lane, sh.count, extra_match,
-                             [&](const u32x4& v, int e) __attribute__((always_inline)) { return ordered(v[e]) == key; });
+  find_and_write<4, false>(a, r, s, 0, rank, prob, kept, wave, lane, sh.small.count, extra_match,
+                           [&](const u32x4& v) __attribute__((always_inline)) {
+                             uint32_t b = 0;
+#pragma unroll
+                             for (int e = 0; e < 4; ++e) b |= ordered(v[e]) == key ? 1u << e : 0u;
+                             return b;
+                           });
 }
 
 }  // namespace
