@@ -151,31 +151,38 @@ __device__ inline __attribute__((always_inline)) void each_held(const u32x4 (&re
     }
 }
 
-// f(j, vector) of the wave's vectors as they lie in memory, four loads ahead: those
-// of the bits of `hits` (j < 64), or, without HITS, all of them.
+// f(j[], vector[]) of the wave's vectors as they lie in memory, four at a time: those
+// of the bits of `hits` (j < 64), or, without HITS, all of them.  (Past the last
+// one: vectors of NaN, j the last one's.)
+constexpr int kBatch = 4;
 template <bool HITS, typename F>
-__device__ inline __attribute__((always_inline)) void visit(const Segment& s, uint64_t hits, int lane, F f) {
-  constexpr int U = 4;
+__device__ inline __attribute__((always_inline)) void visit_batches(const Segment& s, uint64_t hits, int lane, F f) {
   int next = 0;
   while (HITS ? hits != 0 : next * 64 < s.count) {
-    int j[U];
-    u32x4 v[U];
+    int j[kBatch];
+    u32x4 v[kBatch];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
+    for (int i = 0; i < kBatch; ++i) {
+      bool is = true;
       if (HITS) {
-        j[i] = hits ? __builtin_ctzll(hits) : -1;
+        is = hits != 0;
+        j[i] = is ? __builtin_ctzll(hits) : j[i ? i - 1 : 0];
         hits &= hits - 1;
       } else {
-        j[i] = next * 64 < s.count ? next : -1;
-        ++next;
+        j[i] = next++;
       }
       v[i] = u32x4{kNone, kNone, kNone, kNone};
-      if (j[i] >= 0 && j[i] * 64 + lane < s.count) v[i] = s.base[s.first + j[i] * 64 + lane];
+      if (is && j[i] * 64 + lane < s.count) v[i] = s.base[s.first + j[i] * 64 + lane];
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (j[i] >= 0) f(j[i], v[i]);
+    f(j, v);
   }
+}
+template <bool HITS, typename F>
+__device__ inline __attribute__((always_inline)) void visit(const Segment& s, uint64_t hits, int lane, F f) {
+  visit_batches<HITS>(s, hits, lane, [&](const int (&j)[kBatch], const u32x4 (&v)[kBatch]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) f(j[i], v[i]);
+  });
 }
 
 __device__ inline Params params_of(const SampleArgs& a, int r) {
@@ -341,19 +348,21 @@ __device__ inline __attribute__((always_inline)) Found cut_and_draw(const Params
 // of an fp32 lane's).  Up to kCap of them are put in LDS in the order of falling
 // logits and rising index, and every search is one in running sums over that list.
 // ----------------------------------------------------------------------------
-constexpr int kCap = 4096;
+constexpr int kCap = 1024;
 
 struct Small {                   // LDS beside the large arrays
   Sum wave[NW];
   uint32_t count[NW];
   float top[NW];
-  uint32_t tally[2][NW][4];
+  uint32_t tally[2][NW];
   uint32_t listed;
   Found found;
 };
 struct List {
   uint64_t key[kCap];            // falling pattern << 32 | index
   uint64_t sorted[NT];
+  uint32_t index[kCap];
+  uint8_t mask[NW][kRegs][64];   // which of a lane's entries of a vector are candidates
 };
 
 // Bit patterns of fp32 in rising order; -0 as +0.
@@ -436,30 +445,36 @@ __device__ inline __attribute__((always_inline)) float part_maxima_held(const u3
   return block_maximum(m == m ? m : -__builtin_huge_valf(), wave, lane, sm);   // (nothing but NaN: -inf)
 }
 
-// A bound that the k-th largest of the parts' maxima is not below, k <= N * NT: its
-// upper 16 bits, two at a time.
+// A bound that the k-th largest of the parts' maxima is not below, k <= N * NT: a
+// search in the 4096 keys from the row's own down (32 octaves), two bits at a
+// time; the lowest float if it is not among them.  A lane's counts of three
+// thresholds add up in 10 bits each.
 template <int N>
-__device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t k, int wave, int lane, Small& sm) {
-  uint32_t lo = 0;
-  for (int round = 0; round < 8; ++round) {
-    const uint32_t step = 1u << (14 - 2 * round);
+__device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t top_key, uint32_t k, int wave, int lane, Small& sm) {
+  const uint32_t base = top_key > 4095 ? top_key - 4095 : 0;
+  uint32_t lo = base;
+  for (int round = 0; round < 6; ++round) {
+    const uint32_t step = 1u << (10 - 2 * round);
+    uint32_t n = 0;
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-      uint32_t n = 0;
-#pragma unroll
-      for (int i = 0; i < N; ++i) n += __popcll(__ballot(key[i] >= lo + (q + 1) * step));
-      if (lane == 0) sm.tally[round & 1][wave][q] = n;
-    }
+    for (int i = 0; i < N; ++i)
+      n += (key[i] >= lo + step ? 1u : 0u) + (key[i] >= lo + 2 * step ? 1u << 10 : 0u) + (key[i] >= lo + 3 * step ? 1u << 20 : 0u);
+    static_assert(N * 64 < 1024, "counts of a wave in 10 bits");
+    n = count_scan(n);
+    if (lane == 63) sm.tally[round & 1][wave] = n;
     __syncthreads();                             // (the other buffer's readers are past it, too)
-    uint32_t n[3] = {0, 0, 0};
+    uint32_t n1 = 0, n2 = 0, n3 = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w)
-#pragma unroll
-      for (int q = 0; q < 3; ++q) n[q] += sm.tally[round & 1][w][q];
-    lo += (n[0] >= k ? step : 0) + (n[1] >= k ? step : 0) + (n[2] >= k ? step : 0);
+    for (int w = 0; w < NW; ++w) {
+      const uint32_t t = sm.tally[round & 1][w];
+      n1 += t & 1023u;
+      n2 += t >> 10 & 1023u;
+      n3 += t >> 20;
+    }
+    lo += (n1 >= k ? step : 0) + (n2 >= k ? step : 0) + (n3 >= k ? step : 0);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
-  return lo <= kNoKey ? -__FLT_MAX__ : ordered_float(lo << 16);
+  return lo == base || lo <= kNoKey ? -__FLT_MAX__ : ordered_float(lo << 16);
 }
 
 // Draws the row's token from the sorted list and writes it; false if there are too
@@ -475,52 +490,83 @@ __device__ inline __attribute__((always_inline)) bool sample_short(
   // later on).
   auto below = [](double x) { return static_cast<float>(x - fabs(x) * 1e-6); };
   const bool by_min = p.min_p > 0.0 && !(p.top_p < 1.0);
-  const bool by_k = p.top_k && p.top_k <= N * NT && p.top_k <= kCap / 2;
+  const bool by_k = p.top_k && p.top_k <= kCap / 2;
   if (!(p.greedy || by_min || by_k || a.V <= kCap || p.T < 0.05)) return false;
   float bound = top;
   if (!p.greedy && top < __builtin_huge_valf()) {
     bound = fmaxf(below(m - kCut * p.T), -__FLT_MAX__);
     if (by_min) bound = fmaxf(bound, below(m + p.T * log(fmin(p.min_p, 1.0)) - 1e-6 * p.T));
-    if (by_k) bound = fmaxf(bound, kth_bound(key, p.top_k, wave, lane, sm));
+    if (by_k) bound = fmaxf(bound, kth_bound(key, ordered(__float_as_uint(top)) >> 16, p.top_k, wave, lane, sm));
     bound = fminf(bound, top);
   }
   if (tid == 0) sm.listed = 0;
   __syncthreads();
   auto takes = [&](uint32_t bits) { return __uint_as_float(bits) >= bound; };   // (false for NaN)
-  // `b`: which of a lane's entries from `index` on are candidates.
-  auto list_them = [&](uint32_t b, int index, auto bits_of) __attribute__((always_inline)) {
-    const uint32_t own = __popc(b), incl = count_scan(own), total = last_lane(incl);
-    if (total == 0) return;
+  // Room for `own` entries of this lane, at the returned place.
+  auto room = [&](uint32_t own) __attribute__((always_inline)) {
+    const uint32_t incl = count_scan(own), total = last_lane(incl);
     uint32_t at = 0;
-    if (lane == 0) at = atomicAdd(&sm.listed, total);
-    at = __builtin_amdgcn_readfirstlane(at) + incl - own;
-    for (; b; b &= b - 1) {
-      const int e = __builtin_ctz(b);
-      if (at < kCap) list.key[at] = static_cast<uint64_t>(~ordered(bits_of(e))) << 32 | static_cast<uint32_t>(index + e);
-      ++at;
-    }
+    if (total && lane == 0) at = atomicAdd(&sm.listed, total);
+    return __builtin_amdgcn_readfirstlane(at) + incl - own;
   };
-  uint64_t hits = 0;                             // vectors with a candidate in the wave
-  if constexpr (REG)
+  auto put = [&](uint32_t at, int index) {
+    if (at < kCap) list.index[at] = static_cast<uint32_t>(index);
+  };
+  auto mask_of = [&](const u32x4& v) __attribute__((always_inline)) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) b |= takes(entry<BF16>(v, e)) ? 1u << e : 0u;
+    return b;
+  };
+  const bool extra = takes(xbits);
+  if constexpr (REG) {
+    // The masks of the wave's vectors with candidates, one after the other in LDS;
+    // then their indices.
+    uint64_t hits = 0;
+    int n = 0;
     each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
       bool t = false;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) t = t | takes(entry<BF16>(v, e));
-      if (__ballot(t)) hits |= uint64_t{1} << j;
+      if (__ballot(t)) {
+        list.mask[wave][n++][lane] = static_cast<uint8_t>(mask_of(v));
+        hits |= uint64_t{1} << j;
+      }
     });
-  list_them(takes(xbits) ? 1 : 0, s.extra, [&](int) { return xbits; });
-  visit<REG>(s, hits, lane, [&](int j, const u32x4& v) __attribute__((always_inline)) {
-    uint32_t b = 0;
+    uint32_t own = extra ? 1 : 0;
+    for (int i = 0; i < n; ++i) own += __popc(list.mask[wave][i][lane]);
+    uint32_t at = room(own);
+    if (extra) put(at++, s.extra);
+    for (int i = 0; i < n; ++i, hits &= hits - 1) {
+      const int index = s.head + (s.first + __builtin_ctzll(hits) * 64 + lane) * VEC;
+      for (uint32_t b = list.mask[wave][i][lane]; b; b &= b - 1) put(at++, index + __builtin_ctz(b));
+    }
+  } else {
+    const uint32_t first = room(extra ? 1 : 0);
+    if (extra) put(first, s.extra);
+    visit_batches<false>(s, 0, lane, [&](const int (&j)[kBatch], const u32x4 (&v)[kBatch]) __attribute__((always_inline)) {
+      uint32_t b = 0;                            // which entries of the batch
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) b |= takes(entry<BF16>(v, e)) ? 1u << e : 0u;
-    list_them(b, s.head + (s.first + j * 64 + lane) * VEC, [&](int e) {
-      const uint32_t w = v[BF16 ? e / 2 : e];
-      return BF16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w;
+      for (int i = 0; i < kBatch; ++i) b |= mask_of(v[i]) << (i * VEC);
+      if (!__ballot(b != 0)) return;
+      uint32_t at = room(__popc(b));
+      for (; b; b &= b - 1) {
+        const int i = __builtin_ctz(b);
+        put(at++, s.head + (s.first + (j[0] + i / VEC) * 64 + lane) * VEC + i % VEC);
+      }
     });
-  });
+  }
   __syncthreads();
   const int n = static_cast<int>(__builtin_amdgcn_readfirstlane(sm.listed));
   if (n > kCap) return false;
+  const char* row = reinterpret_cast<const char*>(s.base) - s.head * (16 / VEC);   // entry 0
+  for (int i = tid; i < n; i += NT) {
+    const uint32_t index = list.index[i];
+    const uint32_t bits = BF16 ? static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[index]) << 16
+                               : reinterpret_cast<const uint32_t*>(row)[index];
+    list.key[i] = static_cast<uint64_t>(~ordered(bits)) << 32 | index;
+  }
+  __syncthreads();
 
   // In order: by rank where each thread has one candidate, else in pairs.
   const uint64_t* sorted = list.key;
@@ -781,18 +827,13 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
     if (o >= kEndPlace) c[0] = c[1] = 0;
   };
   // Count and weight of one place (0, 0 where it is too far below the top).
+  // (Without a branch: the two places of a lane run side by side.)
   auto place_sum = [&](uint32_t o, uint32_t c, uint64_t* w) __attribute__((always_inline)) {
-    Sum v = {0, 0};
-    *w = 0;
-    if (c) {
-      const double gap = o == top ? 0.0 : place_value(o) - m;
-      if (gap >= -kCut * p.T) {
-        *w = static_cast<uint64_t>(rint(weight(gap, p) * scale));
-        v.n = c;
-        v.z = c * *w;
-      }
-    }
-    return v;
+    const double gap = o == top ? 0.0 : place_value(o) - m;
+    const bool in = c != 0 && gap >= -kCut * p.T;
+    const double x = rint(weight(in ? gap : 0.0, p) * scale);
+    *w = in ? static_cast<uint64_t>(x) : 0;
+    return Sum{in ? c : 0, c * *w};
   };
 
   uint32_t place = top, rank = 0, kept = 1;
