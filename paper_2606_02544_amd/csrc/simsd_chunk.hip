@@ -49,12 +49,40 @@ __device__ inline int visible_keys(const ChunkArgs& a, int kv, int n, int i) {
   return a.mask_block ? min(kv, (pos / a.mask_block + 1) * a.mask_block) : kv;
 }
 
-// Number of the first row block of the sequence that starts at token q0.
+// Number of the first row block of the sequence that starts at token q0, in
+// batches of more than 64.
 __device__ inline int first_block(const ChunkArgs& a, int q0, int b) { return q0 * a.group / a.rows_pb + b; }
 
-// The sequence whose blocks hold number `blk` (one wave; the numbers rise by one a
-// sequence at least, so they are counted 64 at a time).
-__device__ inline int sequence_of_block(const ChunkArgs& a, int blk, int lane) {
+// The sequence and row block of number `blk`; false if there is none.
+//
+// Up to 64 sequences: a lane each; blocks are numbered from the sequence with the
+// most keys down, and from the last rows of each, so that the work-groups with the
+// most work start first and the last ones to start are short.  (24 sequences of 1..351
+// new tokens over 101..6007 keys, 256-row blocks: XX us in the order of the batch, XX
+// in this one.)  More sequences: in the order of the batch from its end, each starting
+// at first_block(), whose numbers rise by one a sequence at least, so that they are
+// counted 64 at a time.
+__device__ inline bool find_block(const ChunkArgs& a, int blk, int lane, Block& w, int* rb) {
+  if (a.batch <= 64) {
+    const int j = min(lane, a.batch - 1);
+    const int q0 = a.q_starts[j], q1 = min(a.q_starts[j + 1], a.tokens), kv = min(max(a.kv_lens[j], 0), a.max_kv);
+    const int nb = lane < a.batch && q1 > q0 ? ((q1 - q0) * a.group + a.rows_pb - 1) / a.rows_pb : 0;
+    int first = 0;                               // blocks of the sequences before this one
+    for (int i = 0; i < a.batch; ++i) {
+      const int k = __builtin_amdgcn_readlane(kv, i), n = __builtin_amdgcn_readlane(nb, i);
+      first += k > kv || (k == kv && i < lane) ? n : 0;
+    }
+    const uint64_t in = __ballot(blk >= first && blk < first + nb);
+    if (!in) return false;
+    const int l = __builtin_ctzll(in);
+    w.b = l;
+    w.q0 = __builtin_amdgcn_readlane(q0, l);
+    w.n = __builtin_amdgcn_readlane(q1, l) - w.q0;
+    w.kv = __builtin_amdgcn_readlane(kv, l);
+    *rb = __builtin_amdgcn_readlane(nb - 1 + first, l) - blk;
+    return w.q0 >= 0;
+  }
+  blk = a.blocks - 1 - blk;
   int n = 0;
   for (int b = 0; b < a.batch; b += 64) {
     const bool at = b + lane < a.batch && first_block(a, a.q_starts[min(b + lane, a.batch - 1)], b + lane) <= blk;
@@ -62,22 +90,23 @@ __device__ inline int sequence_of_block(const ChunkArgs& a, int blk, int lane) {
     n += c;
     if (c < 64) break;
   }
-  return n - 1;
+  if (n == 0) return false;
+  w.b = __builtin_amdgcn_readfirstlane(n - 1);
+  w.q0 = a.q_starts[w.b];
+  w.n = min(a.q_starts[w.b + 1], a.tokens) - w.q0;
+  w.kv = min(max(a.kv_lens[w.b], 0), a.max_kv);
+  *rb = blk - first_block(a, w.q0, w.b);
+  return w.q0 >= 0;
 }
 
 __device__ inline bool setup_block(const ChunkArgs& a, Block& w) {
   w.kvh = blockIdx.x % a.hkv;
-  const int blk = a.blocks - 1 - static_cast<int>(blockIdx.x) / a.hkv;
   w.split = blockIdx.y;
-  w.b = sequence_of_block(a, blk, threadIdx.x & 63);
-  if (w.b < 0) return false;
-  w.b = __builtin_amdgcn_readfirstlane(w.b);
-  w.q0 = a.q_starts[w.b];
-  w.n = min(a.q_starts[w.b + 1], a.tokens) - w.q0;
+  int rb;
+  if (!find_block(a, static_cast<int>(blockIdx.x) / a.hkv, threadIdx.x & 63, w, &rb)) return false;
   w.rows = w.n * a.group;
-  w.row0 = (blk - first_block(a, w.q0, w.b)) * a.rows_pb;
-  if (w.q0 < 0 || w.row0 >= w.rows) return false;
-  w.kv = min(max(a.kv_lens[w.b], 0), a.max_kv);
+  w.row0 = rb * a.rows_pb;
+  if (w.row0 >= w.rows) return false;
   const int last = min(w.row0 + a.rows_pb, w.rows) - 1;
   const int seen = visible_keys(a, w.kv, w.n, last / a.group);
   w.nsplit = max(1, (seen + a.chunk - 1) / a.chunk);
@@ -96,19 +125,33 @@ __device__ inline int64_t partial_row(const ChunkArgs& a, int split, int token, 
 // ----------------------------------------------------------------------------
 // bf16 MFMA kernel
 // ----------------------------------------------------------------------------
-// Streams 64-key K/V tiles of a key range into a ring of LDS tile slots with direct
+// Tiles in LDS: bf16, 64 keys, swizzled for the transpose reads; fp32, 32 keys, chunk
+// c of row r at c ^ (r mod 8), so that the eight rows that eight lanes read at one
+// chunk lie in different banks.
+template <int D>
+struct Bf16Tile {
+  static constexpr int KEYS = kTile, ROWB = TileGeom<D>::ROWB, ELEM = 2;
+  static __device__ inline int swizzle(int r) { return swz<D>(r); }
+};
+template <int D>
+struct F32Tile {
+  static constexpr int KEYS = 32, ROWB = 4 * D, ELEM = 4;
+  static __device__ inline int swizzle(int r) { return r & 7; }
+};
+
+// Streams K/V tiles of a key range into a ring of LDS tile slots with direct
 // loads, split between the waves by instruction.  One instruction covers RPI key
 // rows of one tensor; lane i writes chunk position i % CPR of row i / CPR of its
 // block and so fetches logical chunk (i % CPR) ^ swz(row).  Full tiles take a
 // wave-uniform base an instruction plus a fixed lane offset (paged: an instruction's
 // rows lie in one page when RPI divides the page size); other tiles, and rows past
 // the range's last key, which read that key instead, an address a lane.
-template <int D, int NW, bool PAGED>
+template <typename Tile, int NW, bool PAGED>
 struct ChunkRing {
-  static constexpr int ROWB = TileGeom<D>::ROWB, TILEB = TileGeom<D>::TILEB;
-  static constexpr int CPR = D / 8;            // 16-byte chunks per key row
+  static constexpr int ROWB = Tile::ROWB, KEYS = Tile::KEYS, TILEB = KEYS * ROWB;
+  static constexpr int CPR = ROWB / 16;        // 16-byte chunks per key row
   static constexpr int RPI = 1024 / ROWB;      // key rows per instruction
-  static constexpr int IPT = kTile / RPI;      // instructions per tensor per tile
+  static constexpr int IPT = KEYS / RPI;       // instructions per tensor per tile
   static constexpr int PERW = 2 * IPT / NW;    // instructions per wave per tile
   static_assert(PERW >= 1 && (2 * IPT) % NW == 0, "tile instructions split evenly over the waves");
 
@@ -124,29 +167,29 @@ struct ChunkRing {
   __device__ __attribute__((always_inline)) void init(const ChunkArgs& a, const Block& w, int wave_, int lane_, SIMSD_LDS int* s_pg) {
     wave = wave_;
     lane = lane_;
-    const int64_t hoff = static_cast<int64_t>(w.kvh) * a.cs_head * 2;
+    const int64_t hoff = static_cast<int64_t>(w.kvh) * a.cs_head * Tile::ELEM;
     kc = static_cast<const char*>(a.k_cache) + hoff;
     vc = static_cast<const char*>(a.v_cache) + hoff;
-    tokb = a.cs_tok * 2;
+    tokb = a.cs_tok * Tile::ELEM;
     // Lane offsets of an instruction must fit 32 bits: RPI rows of tokb bytes.
     fast = tokb < (int64_t{1} << 25);
     if (PAGED) {
       P = a.page_size;
       lgP = a.page_shift;
-      pageb = a.cs_seq * 2;
+      pageb = a.cs_seq * Tile::ELEM;
       pg_first = w.kbeg / P;
       const int npg = w.kend > w.kbeg ? (w.kend - 1) / P - pg_first + 1 : 0;   // the plan's chunks: <= kMaxChunkPages
       const int32_t* bt = a.block_table + static_cast<int64_t>(w.b) * a.max_pages + pg_first;
       for (int j = wave * 64 + lane; j < npg; j += NW * 64) s_pg[j] = bt[j];
       fast = fast && P % RPI == 0;
     } else {
-      seqoff = static_cast<int64_t>(w.b) * a.cs_seq * 2;
+      seqoff = static_cast<int64_t>(w.b) * a.cs_seq * Tile::ELEM;
     }
 #pragma unroll
     for (int i = 0; i < PERW; ++i) {
       const int g = wave * PERW + i;
       row[i] = (g % IPT) * RPI + lane / CPR;
-      chunk[i] = (lane % CPR) ^ swz<D>(row[i]);
+      chunk[i] = (lane % CPR) ^ Tile::swizzle(row[i]);
       voff[i] = static_cast<uint32_t>(static_cast<int64_t>(lane / CPR) * tokb + chunk[i] * 16);
     }
   }
@@ -161,7 +204,7 @@ struct ChunkRing {
   // Issue this wave's share of the tile starting at key k0 into the ring slot at
   // LDS byte address `slot`.
   __device__ __attribute__((always_inline)) void issue(uint32_t slot, int k0, int kend, const SIMSD_LDS int* s_pg) const {
-    if (k0 + kTile <= kend && fast) {
+    if (k0 + KEYS <= kend && fast) {
       // Lane j holds the offset of the rows of instruction j of a tensor.
       int64_t at = 0;
       if (PAGED) at = key_offset(k0 + (lane % IPT) * RPI, s_pg);
@@ -227,7 +270,7 @@ __global__ void __launch_bounds__(RW * KW * 64, 2) chunk_bf16_kernel(ChunkArgs a
   constexpr int KS = D / 16;                   // k-steps of QK^T
   constexpr int ROWB = TileGeom<D>::ROWB;
   constexpr int TILEB = TileGeom<D>::TILEB;
-  using Ring = ChunkRing<D, NW, PAGED>;
+  using Ring = ChunkRing<Bf16Tile<D>, NW, PAGED>;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[NBUF][2][TILEB];   // [slot][K, V]
   __shared__ int s_pg_arr[PAGED ? kMaxChunkPages : 1];
   __shared__ int s_bad[2];                     // first and last tile with values that are not finite
@@ -357,8 +400,9 @@ __global__ void __launch_bounds__(RW * KW * 64, 2) chunk_bf16_kernel(ChunkArgs a
         atomicMax(&s_bad[1], it);
       }
       lds_barrier();
-      if (k0 >= wave_end) return;              // no row of this wave sees a key of the tile
     }
+    // No row of this wave sees a key of the tile (or it has no rows).
+    if (k0 >= wave_end) return;
 
 #pragma unroll
     for (int kb1 = 0; kb1 < 2 / KW; ++kb1) {
@@ -787,6 +831,242 @@ __global__ void __launch_bounds__(256, 2) chunk_f32_kernel(ChunkArgs a) {
 }
 
 // ----------------------------------------------------------------------------
+// float32, many rows: four waves of RB 16-row blocks each share tiles of 32 keys in an
+// LDS ring of two slots, two work-groups a CU.  The kernel above reads K and V once
+// per 32 rows from the L2, at 19 TB/s for the chip were its products at their full
+// rate; here it is once per 64 or 128 rows.  What bounds it: the fp32 products.  4 sequences of
+// 512 tokens over 4000 keys, 32/8 heads: 1850 us above, XX us here (floor 928).
+// Operands are as above, read from LDS.
+// ----------------------------------------------------------------------------
+template <int D, int RB, bool PAGED>
+__global__ void __launch_bounds__(256, 2) chunk_f32_rows_kernel(ChunkArgs a) {
+  constexpr int NW = 4, SUB = 16, NBUF = 2;
+  constexpr int KI = D / 16, VU = D / 64;
+  using Ring = ChunkRing<F32Tile<D>, NW, PAGED>;
+  constexpr int ROWB = Ring::ROWB, TILEB = Ring::TILEB, KEYS = Ring::KEYS;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[NBUF][2][TILEB];   // [slot][K, V]
+  __shared__ int s_pg_arr[PAGED ? kMaxChunkPages : 1];
+  __shared__ int s_bad[2];                     // first and last tile with values that are not finite
+  SIMSD_LDS int* s_pg = (SIMSD_LDS int*)(&s_pg_arr[0]);
+
+  Block w;
+  if (!setup_block(a, w)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, q = lane >> 4;
+  if (tid == 0) {
+    s_bad[0] = 0x7fffffff;
+    s_bad[1] = -1;
+  }
+  const int wrow = w.row0 + wave * 16 * RB;    // this wave's first row
+  const int wave_last = min(wrow + 16 * RB, w.rows) - 1;
+  const int wave_end = wrow < w.rows ? visible_keys(a, w.kv, w.n, wave_last / a.group) : 0;
+
+  f32x4 qop[RB][KI];
+  int limit[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    const int m = wrow + 16 * r + n;
+    const int mc = min(m, w.rows - 1), t = mc / a.group;
+    const f32x4* qr = reinterpret_cast<const f32x4*>(
+        static_cast<const float*>(a.q) + (static_cast<int64_t>(w.q0 + t) * a.hq + w.kvh * a.group + mc % a.group) * D);
+#pragma unroll
+    for (int i = 0; i < KI; ++i) qop[r][i] = qr[4 * i + q];
+    limit[r] = m < w.rows ? visible_keys(a, w.kv, w.n, t) : 0;
+  }
+  Ring kv;
+  kv.init(a, w, wave, lane, s_pg);
+  __builtin_amdgcn_s_waitcnt(0);               // (as in the bf16 kernel)
+  __syncthreads();                             // staged page ids, s_bad
+  const int nt = w.kend > w.kbeg ? (w.kend - w.kbeg + KEYS - 1) / KEYS : 0;
+  const uint32_t ring0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((SIMSD_LDS void*)(&smem[0][0][0])));
+  constexpr uint32_t kSlotBytes = 2 * TILEB;
+#pragma unroll
+  for (int j = 0; j < NBUF; ++j)
+    if (j < nt) kv.issue(ring0 + j * kSlotBytes, w.kbeg + j * KEYS, w.kend, s_pg);
+
+  f32x4 o[RB][D / 16];
+  float m_run[RB], l_run[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[r] = kNegInf;
+    l_run[r] = 0.f;
+  }
+  const float sl2 = a.scale_log2;
+  // LDS offsets: K chunk 4 i + q of key n; V chunk 16 u + n of key 4 q + j.
+  auto k_at = [&](const SIMSD_LDS uint8_t* sk, int i) {
+    return *reinterpret_cast<const SIMSD_LDS f32x4*>(sk + n * ROWB + 16 * ((4 * i + q) ^ (n & 7)));
+  };
+  auto v_at = [&](const SIMSD_LDS uint8_t* sv, int j, int u) {
+    const int key = 4 * q + j;
+    return *reinterpret_cast<const SIMSD_LDS f32x4*>(sv + key * ROWB + 16 * ((16 * u + n) ^ (key & 7)));
+  };
+
+  for (int it = 0; it < nt; ++it) {
+    const int k0 = w.kbeg + it * KEYS;
+    if (it == 0 && nt > 1) wait_vm<Ring::PERW>();
+    else wait_vm<0>();
+    lds_barrier();                             // all of tile `it` is in; the other slot is free
+    if (it >= 1 && it + 1 < nt) kv.issue(ring0 + ((it + 1) & 1) * kSlotBytes, k0 + KEYS, w.kend, s_pg);
+    const SIMSD_LDS uint8_t* sk = reinterpret_cast<const SIMSD_LDS uint8_t*>(ring0) + (it & 1) * kSlotBytes;
+    const SIMSD_LDS uint8_t* sv = sk + TILEB;
+    const bool masked = k0 + KEYS > w.full;    // some row of the block does not see all of it
+    if (masked) {
+      bool mine = false;
+#pragma unroll
+      for (int i = 0; i < TILEB / (NW * 64 * 16); ++i) {
+        SIMSD_LDS f32x4* at = (SIMSD_LDS f32x4*)(sv + (i * NW * 64 + tid) * 16);
+        f32x4 x = *at;
+        bool wild = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!(fabsf(x[e]) < __builtin_huge_valf())) {
+            x[e] = 0.f;
+            wild = true;
+          }
+        if (wild) {
+          *at = x;
+          mine = true;
+        }
+      }
+      if (__ballot(mine) && lane == 0) {
+        atomicMin(&s_bad[0], it);
+        atomicMax(&s_bad[1], it);
+      }
+      lds_barrier();
+    }
+#pragma unroll 1
+    for (int sub = 0; sub < KEYS / SUB; ++sub) {
+      const int ks = k0 + SUB * sub;
+      if (ks >= wave_end) break;               // no row of this wave sees a key of it
+      const SIMSD_LDS uint8_t* skb = sk + SUB * sub * ROWB;
+      const SIMSD_LDS uint8_t* svb = sv + SUB * sub * ROWB;
+      f32x4 s[RB];
+#pragma unroll
+      for (int r = 0; r < RB; ++r) s[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {            // four partial sums: shorter rounding chains
+        f32x4 sp[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) sp[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = c * KI / 4; i < (c + 1) * KI / 4; ++i) {
+          const f32x4 kx = k_at(skb, i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+              sp[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qop[r][i][e], sp[r], 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) s[r] += sp[r];
+      }
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (ks + 4 * q + j >= limit[r]) s[r][j] = kNegInf;
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        const float mx = quad_max(fmaxf(fmaxf(s[r][0], s[r][1]), fmaxf(s[r][2], s[r][3])));
+        const float m_new = mx * sl2;
+        if (m_new > m_run[r]) {
+          const float up = ceilf(m_new);
+          const float alpha = __builtin_amdgcn_exp2f(m_run[r] - up);
+          l_run[r] *= alpha;
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) o[r][c] *= alpha;
+          m_run[r] = up;
+        }
+        const float moff = m_run[r] == kNegInf ? 0.f : m_run[r];
+        if (__builtin_expect(__any(fabsf(moff) > 0x1p24f), 0)) {
+#pragma clang fp contract(off)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[r][j] = s[r][j] * sl2 - moff;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[r][j] = fmaf(s[r][j], sl2, -moff);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[r][j] = __builtin_amdgcn_exp2f(s[r][j]);
+          l_run[r] += s[r][j];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+          const f32x4 vx = v_at(svb, j, u);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+              o[r][4 * u + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[e], s[r][j], o[r][4 * u + e], 0, 0, 0);
+        }
+    }
+  }
+  // The tiles with values that are not finite, again.
+  lds_barrier();                               // the ring is free (no load is pending)
+  const int last = __builtin_amdgcn_readfirstlane(s_bad[1]);
+  for (int it = __builtin_amdgcn_readfirstlane(s_bad[0]); it <= last; ++it) {
+    kv.issue(ring0, w.kbeg + it * KEYS, w.kend, s_pg);
+    wait_vm<0>();
+    lds_barrier();
+    const SIMSD_LDS uint8_t* sv = reinterpret_cast<const SIMSD_LDS uint8_t*>(ring0) + TILEB;
+    for (int sub = 0; sub < KEYS / SUB; ++sub) {
+      const int ks = w.kbeg + it * KEYS + SUB * sub;
+#pragma unroll
+      for (int u = 0; u < VU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int r = 0; r < RB; ++r) {
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = v_at(sv + SUB * sub * ROWB, j, u)[e];
+              const float code = fabsf(x) < __builtin_huge_valf() ? 0.f : x > 0.f ? 1.f : x < 0.f ? float(kCode1) : float(kCode2);
+              sum = __builtin_amdgcn_mfma_f32_16x16x4f32(code, ks + 4 * q + j < limit[r] ? 1.f : 0.f, sum, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (sum[i] != 0.f) o[r][4 * u + e][i] += code_value(sum[i]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+    }
+    lds_barrier();
+  }
+
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    const float l = quad_sum(l_run[r]);
+    const int m = wrow + 16 * r + n;
+    if (m >= w.rows) continue;
+    const int t = m / a.group, hq = w.kvh * a.group + m % a.group, token = w.q0 + t;
+    const bool whole = w.nsplit == 1;
+    const int64_t at = whole ? static_cast<int64_t>(token) * a.hq + hq : partial_row(a, w.split, token, hq);
+    const float by = !whole ? 1.f : limit[r] > 0 ? 1.f / l : 0.f;
+    // Register t of o[r][4 u + e] holds dim 64 u + 16 q + 4 t + e of this row.
+    float* x = (whole ? static_cast<float*>(a.out) : a.part) + at * D + 16 * q;
+#pragma unroll
+    for (int u = 0; u < VU; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(x + 64 * u + 4 * i) =
+            f32x4{o[r][4 * u][i], o[r][4 * u + 1][i], o[r][4 * u + 2][i], o[r][4 * u + 3][i]} * by;
+    if (q == 0) {
+      if (!whole) a.part_ml[at] = float2{m_run[r], l};
+      else if (a.lse) a.lse[static_cast<int64_t>(hq) * a.tokens + token] = limit[r] > 0 ? (m_run[r] + __log2f(l)) * kLn2 : kNegInf;
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------
 // Joins the key ranges of a token's rows.  Grid: (token, groups of heads).  D / 4
 // lanes hold a row, four dims each; WIDE: the four waves of a work-group share the
 // ranges of one wave's rows (many ranges), else each has rows of its own.
@@ -885,8 +1165,12 @@ void launch_bf16(const ChunkPlan& p, dim3 grid, const ChunkArgs& a, hipStream_t 
 
 template <int D, bool PAGED>
 void launch_f32(const ChunkPlan& p, dim3 grid, const ChunkArgs& a, hipStream_t st) {
-  if (p.rows_pb == 16) hipLaunchKernelGGL((chunk_f32_kernel<D, 1, PAGED>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((chunk_f32_kernel<D, 2, PAGED>), grid, dim3(256), 0, st, a);
+  switch (p.rows_pb) {
+    case 16: hipLaunchKernelGGL((chunk_f32_kernel<D, 1, PAGED>), grid, dim3(256), 0, st, a); break;
+    case 32: hipLaunchKernelGGL((chunk_f32_kernel<D, 2, PAGED>), grid, dim3(256), 0, st, a); break;
+    case 64: hipLaunchKernelGGL((chunk_f32_rows_kernel<D, 1, PAGED>), grid, dim3(256), 0, st, a); break;
+    default: hipLaunchKernelGGL((chunk_f32_rows_kernel<D, 2, PAGED>), grid, dim3(256), 0, st, a); break;
+  }
 }
 
 template <int D>

@@ -173,7 +173,8 @@ simsd_status plan_chunk(const simsd_chunk_desc* d, int cus, ChunkPlan* p) {
   if (d->kv_chunk < 0 || d->kv_chunk % kTile != 0)
     return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: kv_chunk must be 0 (auto) or a multiple of 64");
   const int64_t strides[3] = {d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head};
-  const simsd_status st = check_strides("chunk_attention", strides, 3, d->dtype == SIMSD_F32 ? 4 : 2, 48);
+  const int eb = d->dtype == SIMSD_F32 ? 4 : 2;
+  const simsd_status st = check_strides("chunk_attention", strides, 3, eb, 48);
   if (st != SIMSD_OK) return st;
   if (!(std::isfinite(d->scale) && d->scale >= 0.f))
     return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: scale must be finite and >= 0");
@@ -181,33 +182,64 @@ simsd_status plan_chunk(const simsd_chunk_desc* d, int cus, ChunkPlan* p) {
   ChunkPlan r;
   r.group = d->num_q_heads / d->num_kv_heads;
   const int64_t rows = int64_t{std::min(d->max_q_len, d->num_tokens)} * r.group;   // of the longest sequence
-  if (d->dtype == SIMSD_BF16) {
-    // Row waves of 32 rows: two (each paired with a wave for the other half of the
-    // keys, two work-groups a CU), four, or eight (one work-group a CU).
-    r.row_waves = rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
-    r.rows_pb = 32 * r.row_waves;
-  } else {
-    r.row_waves = 4;
-    r.rows_pb = rows <= 16 ? 16 : 32;
+  const int64_t tiles = std::max<int64_t>(ceil_div(d->max_kv_len, kTile), 1);
+  int64_t most = tiles * kTile;
+  if (d->page_size > 0)   // a work-group holds the ids of its pages in LDS
+    most = std::min(most, std::max<int64_t>(int64_t{kMaxChunkPages - 1} * d->page_size / kTile * kTile, kTile));
+  // Rows per work-group and key ranges per row: the cheapest by an estimate of the
+  // call's time.  A shape's tile of 64 keys takes `alone` us where its CU has nothing
+  // else, `full` where all slots are taken (D = 128), or what its keys take to come
+  // from memory, which the blocks of a sequence share.  While all work-groups run at
+  // once the longest counts; else what a slot goes through (rows of a chunk see
+  // half of it on average; and a guess, as the lengths are on the device, that the
+  // sequences of a batch have 0.9 of the longest one's keys) and a third of a
+  // work-group for the uneven end.  Joining ranges costs a kernel
+  // and the partials' way to memory and back.
+  //
+  // Calls in us, 32/8 heads, by the shape taken and by others: 64 single tokens over
+  // 512..32767 keys, 64 rows in ranges of 2048 807, whole 949; 8 chunks of 32 tokens over
+  // 4096, 64 rows 41, 128 rows 50 (whole: 69 and 98); 512 tokens over 16000, 256 rows in 4
+  // ranges 163, in 8 172, whole 450, 64 rows 191; a prompt of 2048, 128 rows 59, 256 rows 69,
+  // 64 rows 63; 4 of 2048 over 14336, 256 rows 1990, 128 rows 2114, 64 rows 2560.
+  struct Shape { int row_waves, rows, per_cu; double alone, full; };
+  constexpr Shape kBf16[] = {{2, 64, 2, 0.95, 1.35}, {4, 128, 2, 1.4, 2.2}, {8, 256, 1, 1.8, 2.1}};
+  constexpr Shape kF32[] = {{4, 16, 2, 1.6, 3.2}, {4, 32, 2, 3.2, 6.5}, {4, 64, 2, 6.0, 9.8}, {4, 128, 2, 10.5, 17.4}};
+  const bool bf16 = d->dtype == SIMSD_BF16;
+  const Shape* shapes = bf16 ? kBf16 : kF32;
+  const double scale_d = d->head_dim / 128.0;
+  const double causal = d->mask_block > 0 && d->mask_block < d->max_q_len
+                            ? 1.0 - 0.5 * std::min(d->max_q_len, d->max_kv_len) / std::max(d->max_kv_len, 1) : 1.0;
+  const double even = (d->batch > 1 ? 0.9 : 1.0) * causal;
+  const double part_us = 8.0 * (d->head_dim + 2) * d->num_tokens * d->num_q_heads / 4e6;   // both ways at 4 TB/s
+  int64_t chunk = most;
+  double best = -1.0;
+  for (int i = 0; i < (bf16 ? 3 : 4); ++i) {
+    const Shape& sh = shapes[i];
+    if (i > 0 && shapes[i - 1].rows >= rows) break;   // no sequence fills more than the smaller one
+    const double slots = static_cast<double>(sh.per_cu) * cus;
+    const double blocks = static_cast<double>(ceil_div(ceil_div(int64_t{d->num_tokens} * r.group, d->batch), sh.rows));
+    const double groups = blocks * d->batch * d->num_kv_heads;
+    for (int64_t s = 1; s <= std::min<int64_t>(tiles, 64); s += s < 8 ? 1 : s < 16 ? 2 : s < 32 ? 4 : 8) {
+      const int64_t t = ceil_div(tiles, s);
+      const double x = groups * s / slots;
+      const double cu = x <= 0.5 ? sh.alone : x <= 1.0 ? 0.5 * (sh.alone + sh.full) : sh.full;
+      const double memory = kTile * 2.0 * d->head_dim * eb * std::min(x, 1.0) * slots / 5.5e6 / std::min(blocks, 8.0);
+      const double one = t * std::max(cu * scale_d, memory);
+      double us = x <= 1.0 ? one + 7.0 : even * x * (one + 3.0) + 0.35 * (one + 7.0);
+      if (s > 1) us += 5.0 + s * part_us;
+      if (best < 0.0 || us < best) {
+        best = us;
+        chunk = t * kTile;
+        r.row_waves = sh.row_waves;
+        r.rows_pb = sh.rows;
+      }
+    }
   }
   const int64_t blocks = int64_t{d->num_tokens} * r.group / r.rows_pb + d->batch;
   if (blocks * d->num_kv_heads > (1 << 22))
     return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: too many tokens and sequences for one call");
   r.blocks = static_cast<int>(blocks);
-  // Keys per work-group: all of a row's, unless there are too few row blocks to
-  // fill the chip.
-  const int64_t slots = (r.row_waves >= 4 && d->dtype == SIMSD_BF16 ? 1 : 2) * int64_t{cus};
-  const int64_t groups = blocks * d->num_kv_heads;
-  int64_t most = std::max<int64_t>(ceil_div(d->max_kv_len, kTile) * kTile, kTile);
-  if (d->page_size > 0)   // a work-group holds the ids of its pages in LDS
-    most = std::min(most, std::max<int64_t>(int64_t{kMaxChunkPages - 1} * d->page_size / kTile * kTile, kTile));
-  int64_t chunk = most;
-  if (d->kv_chunk > 0) {
-    chunk = d->kv_chunk;
-  } else if (groups < 4 * slots) {
-    chunk = ceil_div(ceil_div(int64_t{d->max_kv_len} * groups, 4 * slots), kTile) * kTile;
-    chunk = std::max<int64_t>(chunk, 256);
-  }
+  if (d->kv_chunk > 0) chunk = d->kv_chunk;
   chunk = std::min(chunk, most);
   r.chunk = static_cast<int>(chunk);
   r.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(d->max_kv_len, chunk)));

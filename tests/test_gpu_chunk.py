@@ -121,6 +121,36 @@ def test_every_group_shape(dtype, d, max_q):
         check(s, *call(s, mask_block=8, max_q_len=max_q, kv_chunk=kv_chunk), 8)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("lens,hq,hkv", [([(1500, 1700)], 32, 8), ([(700, 2000), (1, 900), (400, 400), (90, 2100)], 32, 8)])
+def test_large(dtype, d, page, lens, hq, hkv):
+    """Enough rows for the largest work-groups; a sample of the rows is compared, one
+    by one, and one with the value of a later key infinite."""
+    s = make(lens, hq, hkv, d, dtype, page, 14)
+    out, lse = call(s, mask_block=8)
+    f = lambda x: x.double().numpy()  # noqa: E731
+    g = np.random.RandomState(5)
+    starts, kv = s["starts"].tolist(), s["kv"].tolist()
+    tokens = sorted(set(g.randint(0, s["q"].shape[0], 60).tolist() + [0, starts[-1] - 1] + starts[:-1]))
+    for t in tokens:
+        b = max(i for i in range(len(kv)) if starts[i] <= t < starts[i + 1])
+        n = ref.seen(kv[b], starts[b + 1] - starts[b], t - starts[b], 8)
+        one = dict(s, q=s["q"][t:t + 1], starts=torch.tensor([0] * (b + 1) + [1] * (len(kv) - b)),
+                   kv=torch.tensor([n if i == b else 0 for i in range(len(kv))]))
+        check(one, out[t:t + 1], lse[:, t:t + 1], 0)
+    # A value that only rows from its block on see.
+    at = kv[0] - 300
+    where = (int(s["table"][0, at // page]), at % page) if page else (0, at)
+    s["v"][where[0], where[1], 0, 3] = float("inf")
+    wild, wild_lse = call(s, mask_block=8)
+    first = starts[1] - (kv[0] - at // 8 * 8)                  # first token that sees it
+    heads = hq // hkv
+    assert bool(torch.isinf(wild[first:starts[1], :heads, 3]).all())
+    wild[first:starts[1], :heads, 3] = out[first:starts[1], :heads, 3]
+    assert torch.equal(wild, out) and torch.equal(wild_lse, lse)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_more_new_tokens_than_cached(dtype):
     """Rows at negative positions see nothing."""
