@@ -777,7 +777,7 @@ def rotary(q, k, positions, freq, *, interleaved: bool = False, attn_factor: flo
     with _Launch(dev, stream) as at:
         for i, x in enumerate((q, k)):
             if x is not None and outs[i] is None:
-                outs[i] = torch.empty(x.shape, dtype=dt, device=dev)
+                outs[i] = torch.empty_like(x, memory_format=torch.contiguous_format)
         qs, ks = strides[:4], strides[4:]
         desc = _rotary_desc(T, heads[0], heads[1], d, rot, int(bool(interleaved)), 0, 0, 0, 0, 0,
                             float(attn_factor), qs[0], qs[1], ks[0], ks[1], 0, 0, qs[2], qs[3],
@@ -802,9 +802,22 @@ def _cache_strides(k_cache, v_cache, dtype, device, hkv, d, page_size, max_kv_le
     """Strides and pages per sequence of a call's cache, which passes _check_cache."""
     if max_kv_len <= 0:
         return (0, 0, 0), 0
+    try:
+        shape, st = k_cache.shape, k_cache.stride()
+        ok = (k_cache.dtype is dtype and v_cache.dtype is dtype and k_cache.device == device
+              and v_cache.device == device and v_cache.shape == shape and v_cache.stride() == st
+              and len(shape) == 4 and st[3] == 1 and shape[2] == hkv and shape[3] == d)
+        if ok and page_size > 0:
+            pages = block_table.shape[1]
+            if (shape[1] == page_size and _is(block_table, (batch, pages), torch.int32, device)
+                    and pages * page_size >= max_kv_len):
+                return st[:3], pages
+        elif ok and shape[0] == batch and shape[1] >= max_kv_len:
+            return st[:3], 0
+    except (AttributeError, TypeError, ValueError, IndexError):
+        pass
     _check_cache(k_cache, v_cache, dtype, device, hkv, d, page_size, max_kv_len, batch, block_table)
-    st = k_cache.stride()
-    return st[:3], block_table.shape[1] if page_size > 0 else 0
+    return k_cache.stride()[:3], block_table.shape[1] if page_size > 0 else 0
 
 
 def rotary_append(q, k, v, k_cache, v_cache, block_table, q_starts, kv_lens, freq, *,
@@ -839,7 +852,7 @@ def rotary_append(q, k, v, k_cache, v_cache, block_table, q_starts, kv_lens, fre
         _vector("positions", positions, T, torch.int32, dev)
     with _Launch(dev, stream) as at:
         if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         desc = _rotary_desc(T, hq, hkv, d, rot, int(bool(interleaved)), b, max_kv_len, page_size, pages,
                             k_cache.shape[0] if pages else 0, float(attn_factor), qs[0], qs[1],
                             ks[0], ks[1], vs[0], vs[1], qo[0], qo[1], 0, 0, cs[0], cs[1], cs[2],
@@ -898,7 +911,7 @@ def chunk_attention(q, k_cache, v_cache, block_table, q_starts, kv_lens, *, max_
         _tensor("lse", lse, (hq, T), torch.float32, dev)
     with _Launch(dev, stream) as at:
         if out is None:
-            out = torch.empty(q.shape, dtype=dt, device=dev)
+            out = torch.empty_like(q)
         if lse is None and want_lse:
             lse = torch.empty((hq, T), dtype=torch.float32, device=dev)
         desc, nbytes = _chunk_desc(dev, T, b, hq, hkv, d, max_q_len, max_kv_len, mask_block, page_size,
@@ -947,9 +960,9 @@ def sample(logits, uniforms, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, 
         else:
             numbers[i] = operator.index(x) if kind is torch.int32 else float(x)
     with _Launch(dev, stream) as at:
-        token = _given("token", token, (n,), torch.int32, dev)
-        prob = _given("prob", prob, (n,), torch.float32, dev)
-        kept = _given("kept", kept, (n,), torch.int32, dev)
+        token = torch.empty_like(uniforms, dtype=torch.int32) if token is None else _given("token", token, (n,), torch.int32, dev)
+        prob = torch.empty_like(uniforms) if prob is None else _given("prob", prob, (n,), torch.float32, dev)
+        kept = torch.empty_like(token) if kept is None else _given("kept", kept, (n,), torch.int32, dev)
         desc = _sample_desc(n, V, *numbers, _dtype_code(dt))
         _check(lib().simsd_sample(ctypes.byref(desc), logits.data_ptr(), uniforms.data_ptr(),
                                   *map(_addr, rows), token.data_ptr(), prob.data_ptr(),

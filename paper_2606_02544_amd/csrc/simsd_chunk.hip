@@ -904,6 +904,7 @@ __global__ void __launch_bounds__(256, 2) chunk_f32_rows_kernel(ChunkArgs a) {
     return *reinterpret_cast<const SIMSD_LDS f32x4*>(sv + key * ROWB + 16 * ((16 * u + n) ^ (key & 7)));
   };
 
+#pragma unroll 1
   for (int it = 0; it < nt; ++it) {
     const int k0 = w.kbeg + it * KEYS;
     if (it == 0 && nt > 1) wait_vm<Ring::PERW>();
@@ -1013,11 +1014,13 @@ __global__ void __launch_bounds__(256, 2) chunk_f32_rows_kernel(ChunkArgs a) {
   // The tiles with values that are not finite, again.
   lds_barrier();                               // the ring is free (no load is pending)
   const int last = __builtin_amdgcn_readfirstlane(s_bad[1]);
+#pragma unroll 1
   for (int it = __builtin_amdgcn_readfirstlane(s_bad[0]); it <= last; ++it) {
     kv.issue(ring0, w.kbeg + it * KEYS, w.kend, s_pg);
     wait_vm<0>();
     lds_barrier();
     const SIMSD_LDS uint8_t* sv = reinterpret_cast<const SIMSD_LDS uint8_t*>(ring0) + TILEB;
+#pragma unroll 1
     for (int sub = 0; sub < KEYS / SUB; ++sub) {
       const int ks = w.kbeg + it * KEYS + SUB * sub;
 #pragma unroll

@@ -203,7 +203,7 @@ simsd_status plan_chunk(const simsd_chunk_desc* d, int cus, ChunkPlan* p) {
   // 64 rows 63; 4 of 2048 over 14336, 256 rows 1990, 128 rows 2114, 64 rows 2560.
   struct Shape { int row_waves, rows, per_cu; double alone, full; };
   constexpr Shape kBf16[] = {{2, 64, 2, 0.95, 1.35}, {4, 128, 2, 1.4, 2.2}, {8, 256, 1, 1.8, 2.1}};
-  constexpr Shape kF32[] = {{4, 16, 2, 1.6, 3.2}, {4, 32, 2, 3.2, 6.5}, {4, 64, 2, 6.0, 9.8}, {4, 128, 2, 10.5, 17.4}};
+  constexpr Shape kF32[] = {{4, 16, 2, 2.0, 3.25}, {4, 32, 2, 4.2, 5.1}, {4, 64, 2, 5.2, 9.2}, {4, 128, 2, 10.4, 17.4}};
   const bool bf16 = d->dtype == SIMSD_BF16;
   const Shape* shapes = bf16 ? kBf16 : kF32;
   const double scale_d = d->head_dim / 128.0;
