@@ -58,7 +58,7 @@ __device__ inline int first_block(const ChunkArgs& a, int q0, int b) { return q0
 // Up to 64 sequences: a lane each; blocks are numbered from the sequence with the
 // most keys down, and from the last rows of each, so that the work-groups with the
 // most work start first and the last ones to start are short.  (24 sequences of 1..351
-// new tokens over 101..6007 keys, 256-row blocks: XX us in the order of the batch, XX
+// new tokens over 101..6007 keys, 256-row blocks: 360 us in the order of the batch, 304
 // in this one.)  More sequences: in the order of the batch from its end, each starting
 // at first_block(), whose numbers rise by one a sequence at least, so that they are
 // counted 64 at a time.
@@ -835,7 +835,8 @@ __global__ void __launch_bounds__(256, 2) chunk_f32_kernel(ChunkArgs a) {
 // LDS ring of two slots, two work-groups a CU.  The kernel above reads K and V once
 // per 32 rows from the L2, at 19 TB/s for the chip were its products at their full
 // rate; here it is once per 64 or 128 rows.  What bounds it: the fp32 products.  4 sequences of
-// 512 tokens over 4000 keys, 32/8 heads: 1850 us above, XX us here (floor 928).
+// 512 tokens over 4000 keys, 32/8 heads: 1379 us with the kernel above, 1240 here
+// (floor 928); a prompt of 4096: 1335 above, 1224 here (64 rows; floor 894).
 // Operands are as above, read from LDS.
 // ----------------------------------------------------------------------------
 template <int D, int RB, bool PAGED>

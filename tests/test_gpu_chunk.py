@@ -94,13 +94,13 @@ def test_shapes(dtype, d, page, lens, hq, hkv):
         check(s, *call(s, mask_block=mask_block), mask_block)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
 @pytest.mark.parametrize("page", [0, 1, 4, 5, 24, 64, 100, 128, 256])
 @pytest.mark.parametrize("kv_chunk", [0, 64, 128])
-def test_pages_and_key_ranges(dtype, page, kv_chunk):
+def test_pages_and_key_ranges(dtype, d, page, kv_chunk):
     """Page sizes that divide a tile, hold several, end inside one or share none of
     its factors; ranges of keys joined by the second kernel."""
-    s = make([(7, 450), (40, 257), (1, 64)], 4, 2, 128, dtype, page, 2)
+    s = make([(7, 450), (40, 257), (1, 64)], 4, 2, d, dtype, page, 2)
     check(s, *call(s, mask_block=4, kv_chunk=kv_chunk), 4)
 
 
@@ -122,11 +122,12 @@ def test_every_group_shape(dtype, d, max_q):
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
-@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("page", [0, 1, 5, 16, 96])
 @pytest.mark.parametrize("lens,hq,hkv", [([(1500, 1700)], 32, 8), ([(700, 2000), (1, 900), (400, 400), (90, 2100)], 32, 8)])
 def test_large(dtype, d, page, lens, hq, hkv):
-    """Enough rows for the largest work-groups; a sample of the rows is compared, one
-    by one, and one with the value of a later key infinite."""
+    """Enough rows for the largest work-groups (pages of one token: more of them than a
+    work-group holds); a sample of the rows is compared, one by one, and one with the
+    value of a later key infinite."""
     s = make(lens, hq, hkv, d, dtype, page, 14)
     out, lse = call(s, mask_block=8)
     f = lambda x: x.double().numpy()  # noqa: E731
@@ -174,10 +175,23 @@ def test_rows_outside_the_batch_stay(dtype, kv_chunk):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("page", [0, 16])
-def test_many_sequences_and_strides(dtype, page):
-    lens = [(1 + i % 3, 1 + i % 3 + (37 * i) % 90) for i in range(150)]
-    s = make(lens, 4, 2, 64, dtype, page, 7, order="htd")
-    check(s, *call(s, mask_block=1), 1)
+@pytest.mark.parametrize("batch,first", [(64, 3), (65, 3), (150, 0)])
+def test_many_sequences_and_strides(dtype, page, batch, first):
+    lens = [(i % 4, i % 4 + (37 * i) % 90) for i in range(batch)]
+    s = make(lens, 4, 2, 64, dtype, page, 7, first=first, pad=first, order="htd")
+    for kv_chunk in (0, 64):
+        check(s, *call(s, mask_block=1, kv_chunk=kv_chunk), 1)
+
+
+def test_one_cache_for_all_sequences():
+    """A cache expanded over the batch (stride 0): a shared prompt."""
+    s = make([(3, 80), (2, 80)], 4, 2, 64, "bf16", 0, 15)
+    s["k"], s["v"] = (x[:1].expand(2, -1, -1, -1) for x in (s["k"], s["v"]))
+    from paper_2606_02544_amd import binding
+    k, v = (s[n][:1].cuda().expand(2, -1, -1, -1) for n in ("k", "v"))
+    out, lse = binding.chunk_attention(s["q"].cuda(), k, v, None, s["starts"].cuda(), s["kv"].cuda(), max_q_len=3,
+                                       max_kv_len=80)
+    check(s, out, lse, 1)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

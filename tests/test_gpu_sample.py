@@ -174,6 +174,30 @@ def test_the_same_on_every_run_and_from_a_graph(dtype):
         u.copy_(torch.rand(9, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_vocabulary(dtype):
+    """2^22 entries: flat, masked with the lowest value, and few of them possible."""
+    x, u = rows(3, 2 ** 22, DT[dtype], 31)
+    x[1] = torch.finfo(DT[dtype]).min
+    x[1, 12345::70001] = 3.0
+    x[2] = 1.0
+    run(x, u)
+    run(x, u, 0.9, 300, 0.9, 0.01)
+    run(x, u, 0.5, 0, 0.3)
+
+
+def test_a_row_past_32_bits_of_offset():
+    """Logits of more than 2^32 bytes: the last rows are read where they lie."""
+    from paper_2606_02544_amd import binding
+    V, n = 2 ** 22, 520
+    x = torch.zeros((n, V), dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 2 ** 31
+    x[n - 1, 77] = x[n - 2, V - 1] = 50.0
+    token, prob, kept = binding.sample(x, torch.full((n,), 0.5, device="cuda"), top_k=5)
+    assert token[n - 1] == 77 and token[n - 2] == V - 1 and kept[0] == 5 and token[0] == 2
+    assert prob[n - 1] == 1.0 and abs(float(prob[0]) - 0.2) < 1e-6
+
+
 def test_given_outputs_and_no_rows():
     from paper_2606_02544_amd import binding
     x, u = rows(2, 100, torch.float32, 1)
