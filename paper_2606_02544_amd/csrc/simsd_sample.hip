@@ -20,10 +20,12 @@
 // bf16 rows: a logit is one of 65536 bit patterns, so one histogram of counts
 // holds the row: 16-bit counters, two to an LDS word, 128 KB.  The row stays in
 // registers (8 waves x 38 loads of 16 bytes a lane, up to 155648 entries; a longer
-// row is read again), is read from memory once,
-// and the weights are taken of the distinct values only (some 3000 of a row of
-// 151936 logits N(0, 4)).  A counter that passes 65535 shows in the total and
-// the histogram is built again, noting each wrap.
+// row is read again), is read from memory once, and the weights are taken of the
+// distinct values only (some 3000 of a row of 151936 logits N(0, 4)).  A counter that
+// passes 65535 shows in the total and the histogram is built again, noting each wrap.
+// What bounds a row is one work-group's LDS and issue, not memory: of the 33 us of a
+// row of 151936, 3 are the read, 15 the counting (2432 LDS atomics of a wave, 15
+// cycles each), 5 the weights, the rest the cuts and the token's index.
 // fp32 rows: the weights are added up in 8192 bins of the upper 13 bits of the
 // ordered bit pattern; a search goes on in the bin it ends in, 10 and then 9
 // bits further, over the row again, which the caches hold by then.
@@ -40,7 +42,7 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int NT = 512;          // threads of a work-group
 constexpr int NW = NT / 64;
-constexpr int kRegs = 38;        // 16-byte loads of a bf16 row that a lane keeps
+constexpr int kRegs = 38;        // 16-byte loads of a bf16 row that a lane keeps; even
 constexpr double kCut = 700.0;   // a token further below the maximum, in temperatures, is never kept
 
 struct Params {
@@ -346,7 +348,10 @@ __device__ inline __attribute__((always_inline)) Found cut_and_draw(const Params
 // top_p is off; and the k-th largest of the maxima of the row's parts (k parts
 // hold an entry not below it; a part is an eighth of a bf16 lane's entries, a quarter
 // of an fp32 lane's).  Up to kCap of them are put in LDS in the order of falling
-// logits and rising index, and every search is one in running sums over that list.
+// logits and rising index, and every search is one in running sums over that list; a
+// row with more goes the long way below.  Per call, long way -> short way: 4 bf16 rows
+// of 151936 with k = 50, 57 -> 17 us; 61 fp32 rows of 50001 with min_p 0.02, 80 ->
+// 22 us; 512 bf16 rows with settings of all kinds, 121 -> 93 us.
 // ----------------------------------------------------------------------------
 constexpr int kCap = 1024;
 
@@ -381,10 +386,23 @@ __device__ inline uint32_t entry(const u32x4& v, int e) {
   else return v[e];
 }
 
-// The largest of the lane's maxima over the work-group.
+template <int CTRL, int ROWS>
+__device__ inline float max_moved(float v) {
+  const int b = __builtin_bit_cast(int, v);
+  return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CTRL, ROWS, 0xf, false)));
+}
+// The largest of the lane's maxima over the wave, and over the work-group.
+__device__ inline float wave_maximum(float m) {
+  m = max_moved<0x111, 0xf>(m);
+  m = max_moved<0x112, 0xf>(m);
+  m = max_moved<0x114, 0xf>(m);
+  m = max_moved<0x118, 0xf>(m);
+  m = max_moved<0x142, 0xa>(m);
+  m = max_moved<0x143, 0xc>(m);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), 63));
+}
 __device__ inline float block_maximum(float m, int wave, int lane, Small& sm) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  m = wave_maximum(m);
   if (lane == 0) sm.top[wave] = m;
   __syncthreads();
 #pragma unroll
@@ -392,8 +410,8 @@ __device__ inline float block_maximum(float m, int wave, int lane, Small& sm) {
   return m;
 }
 
-// Maxima of this lane's parts of the row: key[i] the upper 16 bits of ordered(),
-// and the row's largest entry (-inf if it has none that is a number).
+// Maxima of this lane's parts of the row: key[i] the upper 16 bits of ordered(); and
+// the row's largest entry (-inf where there is none that is a number).
 constexpr uint32_t kNoKey = 0x7f;                // of -inf
 template <bool BF16>
 __device__ inline __attribute__((always_inline)) float part_maxima_read(const Segment& s, uint32_t xbits, int wave, int lane, Small& sm,
@@ -416,20 +434,25 @@ __device__ inline __attribute__((always_inline)) float part_maxima_read(const Se
 }
 // bf16 in registers: two entries at a time as 16-bit integers in the order of their
 // values; NaN of positive sign would be the largest, and sends the row to the other
-// form (*odd).
+// form (*odd).  `pair`: the maxima of two vectors each, even and odd entries apart.
+constexpr int kPairs = kRegs / 2;
 __device__ inline __attribute__((always_inline)) float part_maxima_held(const u32x4 (&reg)[kRegs], const Segment& s, uint32_t xbits,
-                                                                       int wave, int lane, Small& sm, uint32_t (&key)[8], bool* odd) {
+                                                                       int wave, int lane, Small& sm, uint32_t (&key)[8],
+                                                                       s16x2 (&pair)[kPairs], bool* odd) {
   s16x2 part[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) part[i] = s16x2{-0x8000, -0x8000};
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) pair[i] = s16x2{-0x8000, -0x8000};
   auto rising = [](uint32_t w) {
     const s16x2 x = __builtin_bit_cast(s16x2, w);
     return x ^ ((x >> s16x2{15, 15}) & s16x2{0x7fff, 0x7fff});
   };
-  part[0] = __builtin_elementwise_max(part[0], rising(xbits >> 16 | xbits));   // (either half: the entry itself, or 0xffff)
+  part[0] = rising(xbits >> 16 | xbits);         // (either half: the entry itself, or 0xffff)
   each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) part[j % 4] = __builtin_elementwise_max(part[j % 4], rising(v[q]));
+    for (int q = 0; q < 4; ++q) pair[j / 2] = __builtin_elementwise_max(pair[j / 2], rising(v[q]));
+    if (j % 2) part[j / 2 % 4] = __builtin_elementwise_max(part[j / 2 % 4], pair[j / 2]);
   });
   int best = -0x8000;
 #pragma unroll
@@ -440,26 +463,29 @@ __device__ inline __attribute__((always_inline)) float part_maxima_held(const u3
   }
   // Back to the pattern: non-negative ones are themselves.
   const uint32_t bits = static_cast<uint32_t>(best >= 0 ? best : best ^ 0x7fff) << 16;
-  *odd = __syncthreads_or(best > 0x7f80) != 0;
   const float m = __uint_as_float(bits);
-  return block_maximum(m == m ? m : -__builtin_huge_valf(), wave, lane, sm);   // (nothing but NaN: -inf)
+  const float top = block_maximum(m == m ? m : -__builtin_huge_valf(), wave, lane, sm);   // (nothing but NaN: -inf)
+  *odd = __syncthreads_or(best > 0x7f80) != 0;
+  return top;
 }
 
 // A bound that the k-th largest of the parts' maxima is not below, k <= N * NT: a
-// search in the 4096 keys from the row's own down (32 octaves), two bits at a
-// time; the lowest float if it is not among them.  A lane's counts of three
-// thresholds add up in 10 bits each.
+// search in the 4096 keys from the row's own down (32 octaves), a quarter of what is
+// left a round (first 64, 256 and 1024 keys, where most rows' end); the lowest
+// float if it is not among them.  A lane's counts of three thresholds add up in 10 bits
+// each.  (A search by each wave for its share of k takes no barriers, but lets in
+// twice the candidates: the same time in all.)
 template <int N>
 __device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t top_key, uint32_t k, int wave, int lane, Small& sm) {
+  static_assert(N * 64 < 1024, "counts of a wave in 10 bits");
   const uint32_t base = top_key > 4095 ? top_key - 4095 : 0;
-  uint32_t lo = base;
-  for (int round = 0; round < 6; ++round) {
-    const uint32_t step = 1u << (10 - 2 * round);
+  uint32_t lo = base, width = 4096;
+  for (int round = 0; width > 1; ++round) {
+    const uint32_t step = width / 4;
+    const uint32_t t1 = round ? lo + step : base + 3072, t2 = round ? lo + 2 * step : base + 3840, t3 = round ? lo + 3 * step : base + 4032;
     uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      n += (key[i] >= lo + step ? 1u : 0u) + (key[i] >= lo + 2 * step ? 1u << 10 : 0u) + (key[i] >= lo + 3 * step ? 1u << 20 : 0u);
-    static_assert(N * 64 < 1024, "counts of a wave in 10 bits");
+    for (int i = 0; i < N; ++i) n += (key[i] >= t1 ? 1u : 0u) + (key[i] >= t2 ? 1u << 10 : 0u) + (key[i] >= t3 ? 1u << 20 : 0u);
     n = count_scan(n);
     if (lane == 63) sm.tally[round & 1][wave] = n;
     __syncthreads();                             // (the other buffer's readers are past it, too)
@@ -471,9 +497,16 @@ __device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t top_key, ui
       n2 += t >> 10 & 1023u;
       n3 += t >> 20;
     }
-    lo += (n1 >= k ? step : 0) + (n2 >= k ? step : 0) + (n3 >= k ? step : 0);
+    if (round) {
+      lo = n3 >= k ? t3 : n2 >= k ? t2 : n1 >= k ? t1 : lo;
+      width = step;
+    } else if (n1 >= k) {                        // (else all 4096 keys are left)
+      lo = n3 >= k ? t3 : n2 >= k ? t2 : t1;
+      width = n3 >= k ? 64 : n2 >= k ? 256 : 1024;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    width = __builtin_amdgcn_readfirstlane(width);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
   return lo == base || lo <= kNoKey ? -__FLT_MAX__ : ordered_float(lo << 16);
 }
 
@@ -482,7 +515,7 @@ __device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t top_key, ui
 template <bool BF16, bool REG, int N>
 __device__ inline __attribute__((always_inline)) bool sample_short(
     const SampleArgs& a, int r, const u32x4 (&reg)[REG ? kRegs : 1], const Segment& s, uint32_t xbits, const Params& p,
-    float u, float top, const uint32_t (&key)[N], int wave, int lane, Small& sm, List& list) {
+    float u, float top, const uint32_t (&key)[N], const s16x2 (&pair)[REG ? kPairs : 1], int wave, int lane, Small& sm, List& list) {
   constexpr int VEC = BF16 ? 8 : 4;
   const int tid = threadIdx.x;
   const double m = static_cast<double>(top);
@@ -502,7 +535,9 @@ __device__ inline __attribute__((always_inline)) bool sample_short(
   if (tid == 0) sm.listed = 0;
   __syncthreads();
   auto takes = [&](uint32_t bits) { return __uint_as_float(bits) >= bound; };   // (false for NaN)
-  // Room for `own` entries of this lane, at the returned place.
+  // Room for `own` entries of this lane, at the returned place.  (A place taken by
+  // each lane from the counter, and its entries listed where they are found: 13 -> 17
+  // thousand cycles for 60 candidates.)
   auto room = [&](uint32_t own) __attribute__((always_inline)) {
     const uint32_t incl = count_scan(own), total = last_lane(incl);
     uint32_t at = 0;
@@ -521,22 +556,31 @@ __device__ inline __attribute__((always_inline)) bool sample_short(
   const bool extra = takes(xbits);
   if constexpr (REG) {
     // The masks of the wave's vectors with candidates, one after the other in LDS;
-    // then their indices.
+    // then their indices.  (One key lower than the bound's: -0 is not below 0.)
+    const int low = static_cast<int>(ordered(__float_as_uint(bound)) >> 16) - 0x8000 - 2;
+    const int16_t under = static_cast<int16_t>(max(low, -0x8000));
+    const s16x2 none = {under, under};
     uint64_t hits = 0;
     int n = 0;
-    each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
-      bool t = false;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) t = t | takes(entry<BF16>(v, e));
-      if (__ballot(t)) {
-        list.mask[wave][n++][lane] = static_cast<uint8_t>(mask_of(v));
+    for (int i = 0; i < kPairs; ++i) {
+      const uint32_t over = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(pair[i], none));
+      if (!__ballot(over != __builtin_bit_cast(uint32_t, none))) continue;
+#pragma unroll
+      for (int j = 2 * i; j < 2 * i + 2; ++j) {
+        const uint32_t b = mask_of(reg[j]);
+        if (!__ballot(b != 0)) continue;
+        list.mask[wave][n++][lane] = static_cast<uint8_t>(b);
         hits |= uint64_t{1} << j;
       }
-    });
+      __builtin_amdgcn_sched_barrier(0);
+    }
     uint32_t own = extra ? 1 : 0;
+#pragma unroll 4
     for (int i = 0; i < n; ++i) own += __popc(list.mask[wave][i][lane]);
     uint32_t at = room(own);
     if (extra) put(at++, s.extra);
+#pragma unroll 4
     for (int i = 0; i < n; ++i, hits &= hits - 1) {
       const int index = s.head + (s.first + __builtin_ctzll(hits) * 64 + lane) * VEC;
       for (uint32_t b = list.mask[wave][i][lane]; b; b &= b - 1) put(at++, index + __builtin_ctz(b));
@@ -703,23 +747,24 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
   float best;
   if constexpr (REG) {
     uint32_t key[8];
+    s16x2 pair[kPairs];
     bool odd;
-    best = part_maxima_held(reg, s, xbits, wave, lane, sh.small, key, &odd);
-    if (odd) {
+    best = part_maxima_held(reg, s, xbits, wave, lane, sh.small, key, pair, &odd);
+    if (odd) {                                   // (the pairs' maxima let every vector in that holds a NaN)
       uint32_t key4[4];
-      __syncthreads();                           // the first maxima are read
       best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key4);
 #pragma unroll
       for (int i = 0; i < 8; ++i) key[i] = i < 4 ? key4[i] : kNoKey;
     }
     if (best > -__builtin_huge_valf() &&
-        sample_short<true, true>(a, r, reg, s, xbits, p, u, best, key, wave, lane, sh.small, sh.list))
+        sample_short<true, true>(a, r, reg, s, xbits, p, u, best, key, pair, wave, lane, sh.small, sh.list))
       return;
   } else {
     uint32_t key[4];
+    const s16x2 pair[1] = {};
     best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key);
     if (best > -__builtin_huge_valf() &&
-        sample_short<true, false>(a, r, reg, s, xbits, p, u, best, key, wave, lane, sh.small, sh.list))
+        sample_short<true, false>(a, r, reg, s, xbits, p, u, best, key, pair, wave, lane, sh.small, sh.list))
       return;
   }
   if (best == -__builtin_huge_valf()) {
@@ -995,12 +1040,13 @@ __global__ void __launch_bounds__(NT) sample_f32_kernel(SampleArgs a) {
   const float u = a.uniforms[r];
   const u32x4 none[1] = {};                      // (the row is not kept in registers)
   uint32_t part[4];
+  const s16x2 pair[1] = {};
   const float best = part_maxima_read<false>(s, xbits, wave, lane, sh.small, part);
   if (best == -__builtin_huge_valf()) {
     write_none(a, r);
     return;
   }
-  if (sample_short<false, false>(a, r, none, s, xbits, p, u, best, part, wave, lane, sh.small, sh.list)) return;
+  if (sample_short<false, false>(a, r, none, s, xbits, p, u, best, part, pair, wave, lane, sh.small, sh.list)) return;
   __syncthreads();                               // the list's LDS becomes the bins'
   for (int i = tid; i < kBins; i += NT) {
     sh.z[i] = 0;
