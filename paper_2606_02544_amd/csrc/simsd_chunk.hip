@@ -13,7 +13,8 @@
 // with the running maximum and sum, and a second kernel joins them.  Row blocks are
 // numbered without knowing the lengths on the host: sequence b's first block is
 // floor(q_starts[b] * G / R) + b, which leaves room for every sequence's own blocks
-// and at most one unused number a sequence.  KV heads run fastest over the grid, so
+// and at most one unused number a sequence (batches of up to 64 are counted on the
+// device).  KV heads run fastest over the grid, so
 // that the work-groups of one head land on the same XCDs and share their L2; blocks
 // run from the last to the first, the ones with the most keys first.
 //
@@ -102,8 +103,12 @@ __device__ inline bool find_block(const ChunkArgs& a, int blk, int lane, Block& 
 __device__ inline bool setup_block(const ChunkArgs& a, Block& w) {
   w.kvh = blockIdx.x % a.hkv;
   w.split = blockIdx.y;
-  int rb;
-  if (!find_block(a, static_cast<int>(blockIdx.x) / a.hkv, threadIdx.x & 63, w, &rb)) return false;
+  int rb, rank = static_cast<int>(blockIdx.x) / a.hkv;
+  if (a.fold) {
+    const int place = rank, twice = a.blocks - a.fold;   // of the first `fold`, the first `twice` get a second
+    rank = place >= a.fold ? a.blocks - 1 - (place - a.fold) : place < twice ? a.fold - twice + place : place - twice;
+  }
+  if (!find_block(a, rank, threadIdx.x & 63, w, &rb)) return false;
   w.rows = w.n * a.group;
   w.row0 = rb * a.rows_pb;
   if (w.row0 >= w.rows) return false;

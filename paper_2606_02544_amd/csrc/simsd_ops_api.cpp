@@ -162,6 +162,7 @@ extern "C" simsd_status simsd_chunk_attention(const simsd_chunk_desc* desc, cons
     a.max_pages = desc->max_pages_per_seq;
     a.rows_pb = p.rows_pb;
     a.blocks = p.blocks;
+    a.fold = p.fold;
     a.chunk = p.chunk;
     a.scale_log2 = p.scale_log2;
     const hipError_t e = launch_chunk(*desc, p, a, static_cast<hipStream_t>(stream));

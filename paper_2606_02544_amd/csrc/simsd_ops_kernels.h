@@ -42,7 +42,7 @@ struct ChunkArgs {
   float2* part_ml;
   int64_t cs_seq, cs_tok, cs_head;
   int tokens, batch, hq, hkv, group, mask_block, max_kv, page_size, page_shift, max_pages;
-  int rows_pb, blocks, chunk;
+  int rows_pb, blocks, fold, chunk;
   float scale_log2;
 };
 

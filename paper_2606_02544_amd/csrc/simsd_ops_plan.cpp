@@ -146,6 +146,13 @@ simsd_status check_rotary_append_args(const simsd_rotary_desc* d, const void* q,
   return SIMSD_OK;
 }
 
+// Whether row blocks may be put on the CUs by their lengths where the chip holds them
+// all at once, two to a CU: the second one of a CU is the shorter the longer its first
+// (in the order of a longer grid the first half of the blocks, the long ones, all come
+// before a second).  A prompt of 1000 in fp32, 64 rows: 122 -> 103 us; of 2000, 128 rows:
+// 423 -> 335; in bf16, 128 rows: 116.6 -> 114.1.
+static bool may_fold(const simsd_chunk_desc& d, int per_cu) { return per_cu == 2 && d.batch <= 64; }
+
 simsd_status plan_chunk(const simsd_chunk_desc* d, int cus, ChunkPlan* p) {
   if (!d || !p) return fail(SIMSD_ERR_NULL_POINTER, "chunk_attention: descriptor is NULL");
   if (cus < 1) return fail(SIMSD_ERR_HIP, "chunk_attention: the device reports no compute units");
@@ -190,52 +197,67 @@ simsd_status plan_chunk(const simsd_chunk_desc* d, int cus, ChunkPlan* p) {
   // call's time.  A shape's tile of 64 keys takes `alone` us where its CU has nothing
   // else, `full` where all slots are taken (D = 128), or what its keys take to come
   // from memory, which the blocks of a sequence share.  While all work-groups run at
-  // once the longest counts; else what a slot goes through (rows of a chunk see
-  // half of it on average; and a guess, as the lengths are on the device, that the
-  // sequences of a batch have 0.9 of the longest one's keys) and a third of a
-  // work-group for the uneven end.  Joining ranges costs a kernel
-  // and the partials' way to memory and back.
+  // once the slowest CU counts (see may_fold); else what a slot goes through (rows of a
+  // chunk see half of it on average; and a guess, as the lengths are on the device, that
+  // the sequences of a batch have 0.7 of the longest one's keys: ranges cost calls of equal
+  // lengths 5 %, their lack others up to half) and a third of a work-group for the uneven
+  // end.  Joining ranges costs a kernel and the partials' way to memory and back.
   //
-  // Calls in us, 32/8 heads, by the shape taken and by others: 64 single tokens over
-  // 512..32767 keys, 64 rows in ranges of 2048 807, whole 949; 8 chunks of 32 tokens over
-  // 4096, 64 rows 41, 128 rows 50 (whole: 69 and 98); 512 tokens over 16000, 256 rows in 4
-  // ranges 163, in 8 172, whole 450, 64 rows 191; a prompt of 2048, 128 rows 59, 256 rows 69,
-  // 64 rows 63; 4 of 2048 over 14336, 256 rows 1990, 128 rows 2114, 64 rows 2560.
+  // Calls in us, 32/8 heads, by the shape taken and by others.  Single tokens, 64 rows: 64
+  // over 512..32767 keys, ranges of 2048 820, whole 947; 16 over 512..32000, 24 ranges 226,
+  // whole 630; 64 over 4000 each, 3 ranges 206, whole 196.  8 chunks of 32 over 4096, 64 rows
+  // in 3 ranges 43, 128 rows 47 (whole: 68 and 95).  512 tokens over 16000, 128 rows in 4
+  // ranges 158, whole 356, 64 rows 199.  24 of 1..351 over 101..6007, 128 rows 298, 256 rows
+  // 301, 64 rows 370.  A prompt of 2048, 128 rows 56, 256 rows 67, 64 rows 62; 4 of 2048 over
+  // 14336, 256 rows 1970, 128 rows 2050, 64 rows 2510.  fp32: a prompt of 1000, 64 rows 103,
+  // 32 rows 118, 128 rows 138; of 512, 32 rows 36, 64 rows 52; 600 over 2000, 128 rows in 3
+  // ranges 269, 32 rows 250.
   struct Shape { int row_waves, rows, per_cu; double alone, full; };
   constexpr Shape kBf16[] = {{2, 64, 2, 0.95, 1.35}, {4, 128, 2, 1.4, 2.2}, {8, 256, 1, 1.8, 2.1}};
-  constexpr Shape kF32[] = {{4, 16, 2, 2.0, 3.25}, {4, 32, 2, 4.2, 5.1}, {4, 64, 2, 5.2, 9.2}, {4, 128, 2, 10.4, 17.4}};
+  constexpr Shape kF32[] = {{4, 16, 2, 2.0, 3.25}, {4, 32, 2, 3.5, 5.1}, {4, 64, 2, 5.8, 8.2}, {4, 128, 2, 10.4, 17.4}};
   const bool bf16 = d->dtype == SIMSD_BF16;
   const Shape* shapes = bf16 ? kBf16 : kF32;
   const double scale_d = d->head_dim / 128.0;
   const double causal = d->mask_block > 0 && d->mask_block < d->max_q_len
                             ? 1.0 - 0.5 * std::min(d->max_q_len, d->max_kv_len) / std::max(d->max_kv_len, 1) : 1.0;
-  const double even = (d->batch > 1 ? 0.9 : 1.0) * causal;
+  const double even = (d->batch > 1 ? 0.7 : 1.0) * causal;
+  const double least = std::max(2.0 * causal - 1.0, 0.0);   // the shortest block's keys, of the longest one's
   const double part_us = 8.0 * (d->head_dim + 2) * d->num_tokens * d->num_q_heads / 4e6;   // both ways at 4 TB/s
   int64_t chunk = most;
+  int per_cu = 1;
   double best = -1.0;
   for (int i = 0; i < (bf16 ? 3 : 4); ++i) {
     const Shape& sh = shapes[i];
     if (i > 0 && shapes[i - 1].rows >= rows) break;   // no sequence fills more than the smaller one
     const double slots = static_cast<double>(sh.per_cu) * cus;
-    const double blocks = static_cast<double>(ceil_div(ceil_div(int64_t{d->num_tokens} * r.group, d->batch), sh.rows));
+    // Blocks of a sequence: the last one is half full where the lengths differ.
+    const double filled = static_cast<double>(d->num_tokens) * r.group / d->batch / sh.rows;
+    const double blocks = d->batch > 1 ? std::max(filled + 0.5, 1.0) : std::ceil(filled);
     const double groups = blocks * d->batch * d->num_kv_heads;
     for (int64_t s = 1; s <= std::min<int64_t>(tiles, 64); s += s < 8 ? 1 : s < 16 ? 2 : s < 32 ? 4 : 8) {
       const int64_t t = ceil_div(tiles, s);
       const double x = groups * s / slots;
       const double cu = x <= 0.5 ? sh.alone : x <= 1.0 ? 0.5 * (sh.alone + sh.full) : sh.full;
       const double memory = kTile * 2.0 * d->head_dim * eb * std::min(x, 1.0) * slots / 5.5e6 / std::min(blocks, 8.0);
-      const double one = t * std::max(cu * scale_d, memory);
-      double us = x <= 1.0 ? one + 7.0 : even * x * (one + 3.0) + 0.35 * (one + 7.0);
+      double one = t * std::max(cu * scale_d, memory);
+      if (s == 1 && x > 0.5 && x <= 1.0 && may_fold(*d, sh.per_cu)) {
+        const double first = 1.0 - (1.0 / x - 1.0) * (1.0 - least);   // the longest with a second: `least`
+        const double middle = 1.0 - 0.5 / x * (1.0 - least);          // the longest second: as long as its first
+        const double slowest = std::max({sh.alone, sh.alone * (first - least) + sh.full * least, sh.full * middle});
+        one = t * std::max(slowest * scale_d, memory);
+      }
+      double us = x <= 1.0 ? one + 7.0 : even * x * (one + 5.0) + 0.35 * (one + 7.0);
       if (s > 1) us += 5.0 + s * part_us;
       if (best < 0.0 || us < best) {
         best = us;
         chunk = t * kTile;
         r.row_waves = sh.row_waves;
         r.rows_pb = sh.rows;
+        per_cu = sh.per_cu;
       }
     }
   }
-  const int64_t blocks = int64_t{d->num_tokens} * r.group / r.rows_pb + d->batch;
+  const int64_t blocks = std::max<int64_t>(int64_t{d->num_tokens} * r.group - 1, 0) / r.rows_pb + d->batch;
   if (blocks * d->num_kv_heads > (1 << 22))
     return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: too many tokens and sequences for one call");
   r.blocks = static_cast<int>(blocks);
@@ -243,6 +265,8 @@ simsd_status plan_chunk(const simsd_chunk_desc* d, int cus, ChunkPlan* p) {
   chunk = std::min(chunk, most);
   r.chunk = static_cast<int>(chunk);
   r.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(d->max_kv_len, chunk)));
+  const int c = cus / d->num_kv_heads;
+  if (r.splits == 1 && may_fold(*d, per_cu) && r.blocks > c && r.blocks <= 2 * c) r.fold = c;
   if (r.splits > 65535) return fail(SIMSD_ERR_BAD_SHAPE, "chunk_attention: too many key ranges");
   if (r.splits > 1 && d->num_tokens > 0) {
     const size_t n = static_cast<size_t>(r.splits) * d->num_tokens * d->num_q_heads;

@@ -32,7 +32,8 @@ struct ChunkPlan {
   int group = 0;        // Hq / Hkv
   int row_waves = 0;    // bf16: waves that own distinct rows (32 each)
   int rows_pb = 0;      // rows per work-group
-  int blocks = 0;       // row-block numbers: floor(num_tokens * group / rows_pb) + batch
+  int blocks = 0;       // row-block numbers: floor((num_tokens * group - 1) / rows_pb) + batch
+  int fold = 0;         // blocks that start first where the others share their CUs; 0: all the same
   int chunk = 0;        // keys per work-group
   int splits = 0;       // ceil(max_kv_len / chunk), >= 1
   size_t ml_off = 0;    // workspace offset (bytes) of the partial maxima and sums

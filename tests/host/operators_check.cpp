@@ -116,8 +116,11 @@ static int fuzz_chunk() {
   // A work-group's pages fit its LDS.
   if (d.page_size > 0) EXPECT((p.chunk - 1) / d.page_size + 2 <= kMaxChunkPages);
   // Every sequence's blocks have numbers, however the tokens are dealt out: b
-  // sequences of n tokens take at most floor(T G / R) + b blocks.
-  EXPECT(p.blocks == int64_t{d.num_tokens} * p.group / p.rows_pb + d.batch);
+  // sequences of x_i rows (X = T G in all) take sum ceil(x_i / R) <= floor((X - 1) / R) + b
+  // blocks, as ceil(x / R) = floor((x - 1) / R) + 1.
+  EXPECT(p.blocks == std::max<int64_t>(int64_t{d.num_tokens} * p.group - 1, 0) / p.rows_pb + d.batch);
+  // A folded order is one of all blocks: every number once.
+  EXPECT(p.fold == 0 || (p.splits == 1 && p.fold < p.blocks && p.blocks <= 2 * p.fold));
   EXPECT(int64_t{p.blocks} * d.num_kv_heads <= (1 << 22));
   EXPECT(d.dtype == SIMSD_BF16 ? p.rows_pb == 32 * p.row_waves && (p.row_waves == 2 || p.row_waves == 4 || p.row_waves == 8)
                                : p.rows_pb == 16 || p.rows_pb == 32 || p.rows_pb == 64 || p.rows_pb == 128);

@@ -121,6 +121,17 @@ def test_every_group_shape(dtype, d, max_q):
         check(s, *call(s, mask_block=8, max_q_len=max_q, kv_chunk=kv_chunk), 8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", [16, 64])
+@pytest.mark.parametrize("lens", [[(130, 150)], [(256, 256)], [(300, 320)], [(512, 512)], [(900, 900)],
+                                  [(200, 230), (0, 40), (100, 100)], [(64, 64)] * 7 + [(33, 500)]])
+def test_blocks_that_share_a_unit(dtype, heads, lens):
+    """Between one and two row blocks of whole rows a compute unit, in which case they
+    are dealt out by length: every block once."""
+    s = make(lens, heads, heads, 64, dtype, 0, 15)
+    check(s, *call(s, mask_block=8, kv_chunk=1024), 8)
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
 @pytest.mark.parametrize("page", [0, 1, 5, 16, 96])
 @pytest.mark.parametrize("lens,hq,hkv", [([(1500, 1700)], 32, 8), ([(700, 2000), (1, 900), (400, 400), (90, 2100)], 32, 8)])
