@@ -351,7 +351,7 @@ __device__ inline __attribute__((always_inline)) Found cut_and_draw(const Params
 // logits and rising index, and every search is one in running sums over that list; a
 // row with more goes the long way below.  Per call, long way -> short way: 4 bf16 rows
 // of 151936 with k = 50, 57 -> 17 us; 61 fp32 rows of 50001 with min_p 0.02, 80 ->
-// 22 us; 512 bf16 rows with settings of all kinds, 121 -> 93 us.
+// 22 us; 512 bf16 rows with settings of all kinds, 121 -> 90 us.
 // ----------------------------------------------------------------------------
 constexpr int kCap = 1024;
 
@@ -436,6 +436,19 @@ __device__ inline __attribute__((always_inline)) float part_maxima_read(const Se
 // values; NaN of positive sign would be the largest, and sends the row to the other
 // form (*odd).  `pair`: the maxima of two vectors each, even and odd entries apart.
 constexpr int kPairs = kRegs / 2;
+__device__ inline s16x2 rising(uint32_t w) {
+  const s16x2 x = __builtin_bit_cast(s16x2, w);
+  return x ^ ((x >> s16x2{15, 15}) & s16x2{0x7fff, 0x7fff});
+}
+// The row's largest entry from the lanes' largest.
+__device__ inline float row_maximum(int best, int wave, int lane, Small& sm, bool* odd) {
+  // Back to the pattern: non-negative ones are themselves.
+  const uint32_t bits = static_cast<uint32_t>(best >= 0 ? best : best ^ 0x7fff) << 16;
+  const float m = __uint_as_float(bits);
+  const float top = block_maximum(m == m ? m : -__builtin_huge_valf(), wave, lane, sm);   // (nothing but NaN: -inf)
+  *odd = __syncthreads_or(best > 0x7f80) != 0;
+  return top;
+}
 __device__ inline __attribute__((always_inline)) float part_maxima_held(const u32x4 (&reg)[kRegs], const Segment& s, uint32_t xbits,
                                                                        int wave, int lane, Small& sm, uint32_t (&key)[8],
                                                                        s16x2 (&pair)[kPairs], bool* odd) {
@@ -444,10 +457,6 @@ __device__ inline __attribute__((always_inline)) float part_maxima_held(const u3
   for (int i = 0; i < 4; ++i) part[i] = s16x2{-0x8000, -0x8000};
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) pair[i] = s16x2{-0x8000, -0x8000};
-  auto rising = [](uint32_t w) {
-    const s16x2 x = __builtin_bit_cast(s16x2, w);
-    return x ^ ((x >> s16x2{15, 15}) & s16x2{0x7fff, 0x7fff});
-  };
   part[0] = rising(xbits >> 16 | xbits);         // (either half: the entry itself, or 0xffff)
   each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
 #pragma unroll
@@ -461,12 +470,7 @@ __device__ inline __attribute__((always_inline)) float part_maxima_held(const u3
     best = max(best, x);
     key[i] = static_cast<uint32_t>(x + 0x8000);
   }
-  // Back to the pattern: non-negative ones are themselves.
-  const uint32_t bits = static_cast<uint32_t>(best >= 0 ? best : best ^ 0x7fff) << 16;
-  const float m = __uint_as_float(bits);
-  const float top = block_maximum(m == m ? m : -__builtin_huge_valf(), wave, lane, sm);   // (nothing but NaN: -inf)
-  *odd = __syncthreads_or(best > 0x7f80) != 0;
-  return top;
+  return row_maximum(best, wave, lane, sm, odd);
 }
 
 // A bound that the k-th largest of the parts' maxima is not below, k <= N * NT: a
@@ -510,6 +514,13 @@ __device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t top_key, ui
   return lo == base || lo <= kNoKey ? -__FLT_MAX__ : ordered_float(lo << 16);
 }
 
+// Whether a bound worth the look at the parts' maxima is there.
+__device__ inline bool bound_by_min(const Params& p) { return p.min_p > 0.0 && !(p.top_p < 1.0); }
+__device__ inline bool bound_by_k(const Params& p) { return p.top_k && p.top_k <= kCap / 2; }
+__device__ inline bool may_be_short(const Params& p, int V) {
+  return p.greedy || bound_by_min(p) || bound_by_k(p) || V <= kCap || p.T < 0.05;
+}
+
 // Draws the row's token from the sorted list and writes it; false if there are too
 // many candidates (nothing is written then).  N: parts of a lane.
 template <bool BF16, bool REG, int N>
@@ -522,9 +533,8 @@ __device__ inline __attribute__((always_inline)) bool sample_short(
   // The bound, a little lower than it is (weights and cuts are looked at exactly
   // later on).
   auto below = [](double x) { return static_cast<float>(x - fabs(x) * 1e-6); };
-  const bool by_min = p.min_p > 0.0 && !(p.top_p < 1.0);
-  const bool by_k = p.top_k && p.top_k <= kCap / 2;
-  if (!(p.greedy || by_min || by_k || a.V <= kCap || p.T < 0.05)) return false;
+  const bool by_min = bound_by_min(p), by_k = bound_by_k(p);
+  if (!may_be_short(p, a.V)) return false;
   float bound = top;
   if (!p.greedy && top < __builtin_huge_valf()) {
     bound = fmaxf(below(m - kCut * p.T), -__FLT_MAX__);
@@ -744,38 +754,39 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
   if (s.extra >= 0) xbits = static_cast<uint32_t>(static_cast<const uint16_t*>(row)[s.extra]) << 16;
   const Params p = params_of(a, r);
   const float u = a.uniforms[r];
-  float best;
-  if constexpr (REG) {
-    uint32_t key[8];
-    s16x2 pair[kPairs];
-    bool odd;
-    best = part_maxima_held(reg, s, xbits, wave, lane, sh.small, key, pair, &odd);
-    if (odd) {                                   // (the pairs' maxima let every vector in that holds a NaN)
-      uint32_t key4[4];
-      best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key4);
+  // The short way, where there may be one; other rows in registers are counted as
+  // their loads arrive (512 rows with settings of all kinds: 94 -> 90 us).
+  float best = -__builtin_huge_valf();
+  const bool may = !REG || may_be_short(p, a.V);
+  if (may) {
+    if constexpr (REG) {
+      uint32_t key[8];
+      s16x2 pair[kPairs];
+      bool odd;
+      best = part_maxima_held(reg, s, xbits, wave, lane, sh.small, key, pair, &odd);
+      if (odd) {                                 // (the pairs' maxima let every vector in that holds a NaN)
+        uint32_t key4[4];
+        best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key4);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) key[i] = i < 4 ? key4[i] : kNoKey;
+        for (int i = 0; i < 8; ++i) key[i] = i < 4 ? key4[i] : kNoKey;
+      }
+      if (best > -__builtin_huge_valf() &&
+          sample_short<true, true>(a, r, reg, s, xbits, p, u, best, key, pair, wave, lane, sh.small, sh.list))
+        return;
+    } else {
+      uint32_t key[4];
+      const s16x2 pair[1] = {};
+      best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key);
+      if (best > -__builtin_huge_valf() &&
+          sample_short<true, false>(a, r, reg, s, xbits, p, u, best, key, pair, wave, lane, sh.small, sh.list))
+        return;
     }
-    if (best > -__builtin_huge_valf() &&
-        sample_short<true, true>(a, r, reg, s, xbits, p, u, best, key, pair, wave, lane, sh.small, sh.list))
+    if (best == -__builtin_huge_valf()) {
+      write_none(a, r);
       return;
-  } else {
-    uint32_t key[4];
-    const s16x2 pair[1] = {};
-    best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key);
-    if (best > -__builtin_huge_valf() &&
-        sample_short<true, false>(a, r, reg, s, xbits, p, u, best, key, pair, wave, lane, sh.small, sh.list))
-      return;
+    }
+    __syncthreads();                             // the list's LDS becomes the histogram's
   }
-  if (best == -__builtin_huge_valf()) {
-    write_none(a, r);
-    return;
-  }
-  __syncthreads();                               // the list's LDS becomes the histogram's
-  // The largest entry's place (-0 is +0).
-  const uint32_t top = best == 0.f ? kZeroPlace : place_of(__float_as_uint(best) >> 16);
-  const double m = place_value(top);
-  const double scale = a.one;
 
   // One count of a pattern; NOTE: a counter that wraps is noted.
   auto add = [&](uint32_t twice, uint32_t one, auto note) __attribute__((always_inline)) {
@@ -797,6 +808,7 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
       atomicAdd(w, one);
     }
   };
+  s16x2 most = {-0x8000, -0x8000};               // of this lane's entries in registers
   auto build = [&](auto note) __attribute__((always_inline)) {
     u32x4* h = reinterpret_cast<u32x4*>(sh.hist);
     for (int i = tid; i < 32768 / 4; i += NT) h[i] = u32x4{0, 0, 0, 0};
@@ -814,7 +826,12 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
         }
       }
     };
-    if constexpr (REG && !decltype(note)::value) each_held(reg, s, add_all);
+    if constexpr (REG && !decltype(note)::value)
+      each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) most = __builtin_elementwise_max(most, rising(v[q]));
+        add_all(j, v);
+      });
     else visit<false>(s, 0, lane, add_all);
     if (s.extra >= 0) add((xbits >> 15) & 0x1fffcu, 1u << ((xbits >> 12) & 16u), note);
     __syncthreads();
@@ -846,6 +863,23 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
     __syncthreads();
     build(std::true_type{});
   }
+  if (!may) {
+    most = __builtin_elementwise_max(most, rising(xbits >> 16 | xbits));
+    bool odd;
+    best = row_maximum(max(most[0], most[1]), wave, lane, sh.small, &odd);
+    if (odd) {
+      uint32_t key[4];
+      best = part_maxima_read<true>(s, xbits, wave, lane, sh.small, key);
+    }
+    if (best == -__builtin_huge_valf()) {
+      write_none(a, r);
+      return;
+    }
+  }
+  // The largest entry's place (-0 is +0).
+  const uint32_t top = best == 0.f ? kZeroPlace : place_of(__float_as_uint(best) >> 16);
+  const double m = place_value(top);
+  const double scale = a.one;
   // Counts of the places 128 * step + 2 * lane and the next.
   auto counts = [&](uint32_t step, uint32_t (&c)[2]) __attribute__((always_inline)) {
     const uint32_t o = step * 128 + 2 * lane;
