@@ -20,8 +20,17 @@
  *   simsd_verify_accept_sampled  eq. 2 at temperature T: acceptance with
  *                           probability min(1, p_theta/p_phi) and the residual
  *                           draw at the first rejection.
+ * and, for the passes around it:
+ *   simsd_rotary            rotary positions of queries and keys, every layout and
+ *                           scaling of the frequencies;
+ *   simsd_rotary_append     the same, with the keys and values of a ragged batch
+ *                           written to the cache;
+ *   simsd_chunk_attention   block-causal attention of prompts, chunks and single
+ *                           tokens over that cache (no drafts);
+ *   simsd_sample            one token a row from filtered logits: what the drafter
+ *                           proposes, or the target where nothing was drafted.
  *
- * Conventions shared by both calls
+ * Conventions shared by all calls
  * --------------------------------
  *  - Sizes are element counts.  All tensors are row-major and densely packed
  *    unless a stride is given.  "b" = batch index.
@@ -39,9 +48,9 @@
  *    num_ref[b] = gamma_b <= L; reference slots r >= gamma_b are padding.
  *    Each value 1..gamma_b must occur exactly once per sequence; the kernels
  *    do not check this (simsd_validate_step_map does, on the host).
- *  - Every pointer argument of the two compute calls is device memory owned by
+ *  - Every pointer argument of a compute call is device memory owned by
  *    the caller.  The library allocates nothing, frees nothing and never
- *    synchronises: both calls only enqueue work on `stream` (a hipStream_t
+ *    synchronises: a call only enqueues work on `stream` (a hipStream_t
  *    passed as void*; NULL = the default stream) and return.
  *  - Errors: the host checks shapes, dtypes, null pointers, 16-byte alignment
  *    and workspace size before anything is enqueued and returns a status other

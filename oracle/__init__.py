@@ -16,7 +16,12 @@ A plain, slow, float64 numpy statement of what the GPU path computes:
                   (float64) and handed to the greedy acceptance;
   * ``sampled``   the stochastic form of eq. 2 at temperature T: acceptance with
                   probability min(1, p_theta/p_phi) from caller-supplied uniforms
-                  and the residual draw at the first rejection.
+                  and the residual draw at the first rejection;
+  * ``rotary``    rotary positions in every layout, scaled frequencies, and the
+                  cache rows that a ragged batch's new tokens take;
+  * ``chunk``     softmax attention of new tokens under the block-causal mask;
+  * ``sampling``  temperature, top-k, top-p and min-p over a sorted row, and the
+                  draw from a given uniform number.
 
 Only the test-suite, the smoke check and the benchmark's CPU-baseline leg may
 import this package.  The product path (the C-ABI library and its Python

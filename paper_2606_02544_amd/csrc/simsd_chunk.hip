@@ -267,6 +267,10 @@ __device__ inline uint32_t code_of(uint32_t x) {   // one bf16 -> the bf16 code 
 // RW row waves of 32 rows each; KW = 2 pairs every row wave with a second wave that
 // takes the other 32-key half of each tile.  The ring holds NBUF tiles.  (Group
 // shapes and ring depths are the verification attention's, measured there.)
+// What bounds it: with many rows the matrix cores and the softmax between them (4
+// sequences of 2048 tokens over 14336 keys, 32/8 heads of 128: 1970 us, 1050 TFLOP/s; a
+// large matrix product reaches 1133); with few, memory (64 single tokens over 512..32767
+// keys: 812 us, 5.4 TB/s; one block of 4 over 1024 keys: 7 us of round trips).
 template <int D, int RW, int KW, bool PAGED>
 __global__ void __launch_bounds__(RW * KW * 64, 2) chunk_bf16_kernel(ChunkArgs a) {
   constexpr int NW = RW * KW;
@@ -584,6 +588,8 @@ __global__ void __launch_bounds__(RW * KW * 64, 2) chunk_bf16_kernel(ChunkArgs a
 //   O^T += V^T P^T: MFMA j contracts keys 4 {0..3} + j.  Register j of the
 //     scores is key 4 q + j of row n already; the V^T operand is key 4 q + j, dim
 //     64 u + 4 n + e, register e of the 16-byte load (j, u).
+// It serves few rows (8 single tokens over up to 4000 keys, 32/8 heads: 36 us; a prompt of
+// 512: 36 us, of 1000: 118, where the kernel below takes 103).
 // ----------------------------------------------------------------------------
 template <int D, int RB, bool PAGED>
 __global__ void __launch_bounds__(256, 2) chunk_f32_kernel(ChunkArgs a) {
@@ -1078,7 +1084,8 @@ __global__ void __launch_bounds__(256, 2) chunk_f32_rows_kernel(ChunkArgs a) {
 // ----------------------------------------------------------------------------
 // Joins the key ranges of a token's rows.  Grid: (token, groups of heads).  D / 4
 // lanes hold a row, four dims each; WIDE: the four waves of a work-group share the
-// ranges of one wave's rows (many ranges), else each has rows of its own.
+// ranges of one wave's rows (many ranges), else each has rows of its own.  Round trips
+// bound it: 4 tokens in 9 ranges 3.8 us, 64 in 16 ranges 6.
 // ----------------------------------------------------------------------------
 template <int D, bool BF16, bool WIDE>
 __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a) {

@@ -477,8 +477,8 @@ __device__ inline __attribute__((always_inline)) float part_maxima_held(const u3
 // search in the 4096 keys from the row's own down (32 octaves), a quarter of what is
 // left a round (first 64, 256 and 1024 keys, where most rows' end); the lowest
 // float if it is not among them.  A lane's counts of three thresholds add up in 10 bits
-// each.  (A search by each wave for its share of k takes no barriers, but lets in
-// twice the candidates: the same time in all.)
+// each.  (A search by each wave for its share of k takes no barriers, but lets in twice
+// the candidates: 4 rows of 151936, 17.4 -> 19.0 us.)
 template <int N>
 __device__ inline float kth_bound(const uint32_t (&key)[N], uint32_t top_key, uint32_t k, int wave, int lane, Small& sm) {
   static_assert(N * 64 < 1024, "counts of a wave in 10 bits");
