@@ -86,7 +86,7 @@ extern "C" simsd_status simsd_rotary_append(const simsd_rotary_desc* desc, const
     RotaryPlan p;
     simsd_status st = plan_rotary(desc, true, &p);
     if (st == SIMSD_OK)
-      st = check_rotary_append_args(desc, q, k, v, freq, q_out, k_cache, v_cache, block_table,
+      st = check_rotary_append_args(desc, q, k, v, positions, freq, q_out, k_cache, v_cache, block_table,
                                     q_starts, kv_lens);
     if (st != SIMSD_OK || desc->num_tokens == 0) return st;
     int dev = 0, cus = 0;

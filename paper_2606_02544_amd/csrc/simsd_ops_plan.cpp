@@ -122,7 +122,8 @@ simsd_status check_rotary_args(const simsd_rotary_desc* d, const void* q, const 
 }
 
 simsd_status check_rotary_append_args(const simsd_rotary_desc* d, const void* q, const void* k,
-                                      const void* v, const double* freq, const void* q_out,
+                                      const void* v, const int32_t* positions,
+                                      const double* freq, const void* q_out,
                                       const void* k_cache, const void* v_cache,
                                       const int32_t* block_table, const int32_t* q_starts,
                                       const int32_t* kv_lens) {
@@ -139,6 +140,9 @@ simsd_status check_rotary_append_args(const simsd_rotary_desc* d, const void* q,
   for (const void* a : data)
     if (!aligned(a, 16))
       return fail(SIMSD_ERR_ALIGNMENT, "rotary: q, k, v, q_out and the cache must be 16-byte aligned");
+  const void* words[] = {positions, block_table, q_starts, kv_lens};
+  for (const void* a : words)
+    if (!aligned(a, 4)) return fail(SIMSD_ERR_ALIGNMENT, "rotary: int32 arrays must be 4-byte aligned");
   if (!aligned(freq, 8)) return fail(SIMSD_ERR_ALIGNMENT, "rotary: freq must be 8-byte aligned");
   if (d->num_q_heads > 0 && q == q_out &&
       (d->q_stride_token != d->q_out_stride_token || d->q_stride_head != d->q_out_stride_head))

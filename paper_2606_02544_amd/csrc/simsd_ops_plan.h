@@ -22,7 +22,8 @@ simsd_status check_rotary_args(const simsd_rotary_desc* d, const void* q, const 
                                const int32_t* positions, const double* freq, const void* q_out,
                                const void* k_out);
 simsd_status check_rotary_append_args(const simsd_rotary_desc* d, const void* q, const void* k,
-                                      const void* v, const double* freq, const void* q_out,
+                                      const void* v, const int32_t* positions,
+                                      const double* freq, const void* q_out,
                                       const void* k_cache, const void* v_cache,
                                       const int32_t* block_table, const int32_t* q_starts,
                                       const int32_t* kv_lens);

@@ -84,7 +84,7 @@ static int fuzz_rotary() {
   EXPECT(turning * per + (p.q_units - turning) * p.vec == d.head_dim);
   EXPECT(p.units == p.q_units * (d.num_q_heads + d.num_kv_heads) + p.v_units * d.num_kv_heads);
   EXPECT(p.units >= 0 && p.units <= (1 << 26));
-  if (append) check_rotary_append_args(&d, P, P, P, D, P, P, P, I, I, I);
+  if (append) check_rotary_append_args(&d, P, P, P, I, D, P, P, P, I, I, I);
   else check_rotary_args(&d, P, P, I, D, P, P);
   return 1;
 }

@@ -100,7 +100,7 @@ def test_rotary_pointers(no_gpu):
     assert append(rotary_desc(page_size=16, max_pages_per_seq=2, num_pages=4), block_table=NULL) == 1
     for n, at in (("q", 8), ("k_out", 8), ("freq", 4), ("positions", 2)):
         assert rotary(d, **{n: ctypes.c_void_p(0x10000 + at)}) == 4, n
-    for n, at in (("v", 8), ("k_cache", 8), ("freq", 4)):
+    for n, at in (("v", 8), ("k_cache", 8), ("freq", 4), ("positions", 2), ("q_starts", 1), ("kv_lens", 2)):
         assert append(d, **{n: ctypes.c_void_p(0x10000 + at)}) == 4, n
     # in place with other strides
     wide = rotary_desc(q_stride_token=512)
