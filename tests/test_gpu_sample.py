@@ -133,6 +133,25 @@ def test_infinite_and_signed_zero_logits(dtype):
     run(x, u, 1.0, 70, 0.6, 0.5)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [5003, 151936])
+def test_logits_of_one_sign(dtype, V):
+    """Log-probabilities (nothing positive), few positive entries, a NaN among them,
+    and the largest entry at either end of the row."""
+    x, u = rows(6, V, DT[dtype], 40)
+    x[0] -= 40.0
+    x[1] = torch.log_softmax(x[1].float(), 0).to(DT[dtype])
+    x[2, 10:] = -x[2, 10:].abs() - 0.5
+    x[3, V // 2] = float("nan")
+    x[4, 0] = 30.0
+    x[5, V - 1] = 30.0
+    run(x, u)
+    run(x, u, 0.8, 40, 0.9)
+    run(x, u, 1.0, 0, 1.0, 0.05)
+    run(x, u, 1.0, 0, 0.9)
+    run(x, u, 0.0)
+
+
 def test_every_bf16_pattern():
     bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
     g = torch.Generator().manual_seed(3)
