@@ -27,6 +27,7 @@
 
 #include "simsd_device.h"
 #include "simsd_ops_kernels.h"
+#include "simsd_search.h"
 
 namespace simsd {
 namespace {
@@ -61,8 +62,7 @@ __device__ inline int first_block(const ChunkArgs& a, int q0, int b) { return q0
 // most work start first and the last ones to start are short.  (24 sequences of 1..351
 // new tokens over 101..6007 keys, 256-row blocks: 360 us in the order of the batch, 304
 // in this one.)  More sequences: in the order of the batch from its end, each starting
-// at first_block(), whose numbers rise by one a sequence at least, so that they are
-// counted 64 at a time.
+// at first_block(), whose numbers rise by one a sequence at least.
 __device__ inline bool find_block(const ChunkArgs& a, int blk, int lane, Block& w, int* rb) {
   if (a.batch <= 64) {
     const int j = min(lane, a.batch - 1);
@@ -84,13 +84,7 @@ __device__ inline bool find_block(const ChunkArgs& a, int blk, int lane, Block& 
     return w.q0 >= 0;
   }
   blk = a.blocks - 1 - blk;
-  int n = 0;
-  for (int b = 0; b < a.batch; b += 64) {
-    const bool at = b + lane < a.batch && first_block(a, a.q_starts[min(b + lane, a.batch - 1)], b + lane) <= blk;
-    const int c = __popcll(__ballot(at));
-    n += c;
-    if (c < 64) break;
-  }
+  const int n = leading(a.batch, lane, [&](int b) { return first_block(a, a.q_starts[b], b) <= blk; });
   if (n == 0) return false;
   w.b = __builtin_amdgcn_readfirstlane(n - 1);
   w.q0 = a.q_starts[w.b];
@@ -1097,14 +1091,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int token = blockIdx.x;
-  int b = 0;                                   // sequences that end at or before the token
-  for (int i = 0; i < a.batch; i += 64) {
-    const bool before = i + lane < a.batch && a.q_starts[min(i + lane, a.batch - 1) + 1] <= token;
-    const int c = __popcll(__ballot(before));
-    b += c;
-    if (c < 64) break;
-  }
-  b = __builtin_amdgcn_readfirstlane(b);
+  const int b = __builtin_amdgcn_readfirstlane(leading(a.batch, lane, [&](int i) { return a.q_starts[i + 1] <= token; }));
   if (b >= a.batch || token < a.q_starts[0]) return;
   const int q0 = a.q_starts[b], n = min(a.q_starts[b + 1], a.tokens) - q0;
   const int kv = min(max(a.kv_lens[b], 0), a.max_kv);

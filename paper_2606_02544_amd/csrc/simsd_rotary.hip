@@ -14,6 +14,7 @@
 // (32/8 heads of 128, bf16: 32768 tokens into a contiguous cache 157 us, 5.1 TB/s; 4224
 // into pages of 16, 21 us, 4.9 TB/s; 8 tokens 3.2 us.)
 #include "simsd_ops_kernels.h"
+#include "simsd_search.h"
 
 namespace simsd {
 namespace {
@@ -64,16 +65,9 @@ struct Token {
 };
 
 // Sequence of token t: the number of sequences that end at or before it (one
-// wave; starts do not fall, so the ends are counted 64 at a time).
+// wave; starts do not fall).
 __device__ inline int sequence_of(const int32_t* q_starts, int batch, int t, int lane) {
-  int n = 0;
-  for (int b = 0; b < batch; b += 64) {
-    const bool before = b + lane < batch && q_starts[b + lane + 1] <= t;
-    const int c = __popcll(__ballot(before));
-    n += c;
-    if (c < 64) break;
-  }
-  return n;
+  return leading(batch, lane, [&](int b) { return q_starts[b + 1] <= t; });
 }
 
 // Unit u of a token, in order: queries, keys, values.  A turning unit holds VEC

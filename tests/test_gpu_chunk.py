@@ -186,7 +186,7 @@ def test_rows_outside_the_batch_stay(dtype, kv_chunk):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("page", [0, 16])
-@pytest.mark.parametrize("batch,first", [(64, 3), (65, 3), (150, 0)])
+@pytest.mark.parametrize("batch,first", [(64, 3), (65, 3), (150, 0), (130, 1), (4161, 2)])
 def test_many_sequences_and_strides(dtype, page, batch, first):
     lens = [(i % 4, i % 4 + (37 * i) % 90) for i in range(batch)]
     s = make(lens, 4, 2, 64, dtype, page, 7, first=first, pad=first, order="htd")

@@ -106,7 +106,8 @@ def ragged(lens, tokens, first=0):
 @pytest.mark.parametrize("page", [0, 1, 16, 24])
 @pytest.mark.parametrize("lens,kv,first,pad", [
     ([1], [1], 0, 0), ([3, 0, 5, 1], [3, 0, 100, 77], 0, 0), ([0, 0], [5, 0], 2, 3),
-    ([1] * 70, list(range(1, 71)), 1, 2), ([65, 7, 130], [65, 107, 131], 0, 9)])
+    ([1] * 70, list(range(1, 71)), 1, 2),
+    ([i % 3 for i in range(4200)], [i % 3 + i % 131 for i in range(4200)], 2, 1), ([65, 7, 130], [65, 107, 131], 0, 9)])
 def test_append(dtype, d, interleaved, page, lens, kv, first, pad):
     from paper_2606_02544_amd import binding
     hq, hkv, cap = 4, 2, 136
