@@ -461,7 +461,8 @@ __device__ inline __attribute__((always_inline)) float part_maxima_held(const u3
   for (int i = 0; i < 4; ++i) part[i] = s16x2{-0x8000, -0x8000};
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) pair[i] = s16x2{-0x8000, -0x8000};
-  part[0] = rising(xbits >> 16 | xbits);         // (either half: the entry itself, or 0xffff)
+  // (The entry outside the vectors is of one half's part: in both, it would count as two of the k.)
+  part[0] = rising(xbits >> 16 | 0xffff0000u);
   each_held(reg, s, [&](int j, const u32x4& v) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) pair[j / 2] = __builtin_elementwise_max(pair[j / 2], rising(v[q]));
