@@ -724,6 +724,7 @@ __device__ inline __attribute__((always_inline)) bool sample_short(
 // Place of a bit pattern in the falling order: positive ones from the largest
 // (+0 last), then negative ones from -0 on.  -0 counts as +0.
 constexpr uint32_t kInfPlace = 0x7f, kZeroPlace = 0x7fff, kEndPlace = 0xff80;   // +inf; +0; -inf
+constexpr int kMinusZero = 0x8000;              // its pattern
 __device__ inline uint32_t place_bits(uint32_t o) { return o < 0x8000u ? 0x7fffu - o : o; }
 __device__ inline uint32_t place_of(uint32_t bits) { return bits < 0x8000u ? 0x7fffu - bits : bits; }
 __device__ inline double place_value(uint32_t o) { return static_cast<double>(__uint_as_float(place_bits(o) << 16)); }
@@ -856,10 +857,12 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
     if (lane == 0) atomicAdd(&sh.total, sum);
+    // -0 counts in +0's place, whose step is live with it.  (Thread 0 wrote that flag.)
+    if (tid == 0 && (sh.hist[kMinusZero / 2] & 0xffffu)) sh.any[kZeroPlace / 128] = 1;
     __syncthreads();
     if constexpr (decltype(note)::value) {       // counts of 65536 read 0
       for (uint32_t i = tid; i < sh.wraps; i += NT)
-        if (sh.wrap[i] >= 0) sh.any[place_of(sh.wrap[i]) / 128] = 1;
+        if (sh.wrap[i] >= 0) sh.any[sh.wrap[i] == kMinusZero ? kZeroPlace / 128 : place_of(sh.wrap[i]) / 128] = 1;
       __syncthreads();
     }
   };
@@ -902,8 +905,8 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
       }
     }
     if (o + 1 == kZeroPlace) {                   // -0 joins +0
-      c[1] += sh.hist[0x4000] & 0xffffu;
-      for (uint32_t i = 0; i < sh.wraps; ++i) c[1] += sh.wrap[i] == 0x8000 ? 65536 : 0;
+      c[1] += sh.hist[kMinusZero / 2] & 0xffffu;
+      for (uint32_t i = 0; i < sh.wraps; ++i) c[1] += sh.wrap[i] == kMinusZero ? 65536 : 0;
     }
     if (o == kZeroPlace + 1) c[0] = 0;
     if (o < kInfPlace) c[0] = 0;

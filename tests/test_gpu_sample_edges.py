@@ -43,3 +43,43 @@ def test_largest_logits_outside_the_vectors(dtype, V, k):
     run(x.to(DT[dtype]), u, 4.0, k)
     run(x.to(DT[dtype]), u, 4.0, k, 0.9)
     run(x.to(DT[dtype]), u, 4.0, k, 1.0, 0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [1025, 5003, 151936, 200003])
+def test_negative_zeros_without_positive_ones(dtype, V):
+    """Every zero of a row is -0: all entries, the largest one with the rest near or far
+    below, some below positive ones, and none but entries that are never kept beside."""
+    g = torch.Generator().manual_seed(V)
+    x = -torch.randn((7, V), generator=g).abs() - 0.25
+    x[0] = -0.0
+    x[1, V // 3] = -0.0
+    x[2] -= 60.0
+    x[2, 5::701] = -0.0
+    x[3, ::5] = -0.0
+    x[3, 1::5] = 1.5
+    x[4] = float("-inf")
+    x[4, 3::11] = -0.0
+    x[5] = torch.randn(V, generator=g)
+    x[5, 7::13] = -0.0
+    x[6] = float("nan")
+    x[6, ::2] = -0.0
+    assert not (x.view(torch.int32) == 0).any()
+    x, u = x.to(DT[dtype]), torch.rand(7, generator=g)
+    run(x, u)
+    run(x, u, 1.0, 0, 0.9)
+    run(x, u, 0.7, 1000, 0.8)
+    run(x, u, 1.0, 0, 0.95, 0.01)
+    run(x, u, 0.0)
+
+
+@pytest.mark.parametrize("V", [65537, 151936, 2 ** 22])
+@pytest.mark.parametrize("n", [65535, 65536, 65537, 131072])
+def test_counts_of_negative_zeros_past_16_bits(V, n):
+    g = torch.Generator().manual_seed(n)
+    x = -torch.randn((2, V), generator=g).abs() - 0.25
+    x[:, torch.randperm(V, generator=g)[:n]] = -0.0
+    x[1, V - 1] = 1.0
+    x, u = x.bfloat16(), torch.rand(2, generator=g)
+    run(x, u)
+    run(x, u, 1.0, 0, 0.3)
