@@ -724,7 +724,7 @@ __device__ inline __attribute__((always_inline)) bool sample_short(
 // Place of a bit pattern in the falling order: positive ones from the largest
 // (+0 last), then negative ones from -0 on.  -0 counts as +0.
 constexpr uint32_t kInfPlace = 0x7f, kZeroPlace = 0x7fff, kEndPlace = 0xff80;   // +inf; +0; -inf
-constexpr int kMinusZero = 0x8000;              // its pattern
+constexpr int kMinusZero = 0x8000, kMinusInf = 0xff80;   // their patterns
 __device__ inline uint32_t place_bits(uint32_t o) { return o < 0x8000u ? 0x7fffu - o : o; }
 __device__ inline uint32_t place_of(uint32_t bits) { return bits < 0x8000u ? 0x7fffu - bits : bits; }
 __device__ inline double place_value(uint32_t o) { return static_cast<double>(__uint_as_float(place_bits(o) << 16)); }
@@ -794,6 +794,11 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
     __syncthreads();                             // the list's LDS becomes the histogram's
   }
 
+  // NaN of negative sign counts as -inf: neither is ever kept.
+  auto counted = [](uint32_t w) __attribute__((always_inline)) {
+    const u16x2 least = {kMinusInf, kMinusInf};
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, w), least));
+  };
   // One count of a pattern; NOTE: a counter that wraps is noted.
   auto add = [&](uint32_t twice, uint32_t one, auto note) __attribute__((always_inline)) {
     // twice: byte offset of the pattern's word; one: 1 in its half
@@ -827,8 +832,9 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
       if ((v[0] & v[1] & v[2] & v[3]) != kNone) {   // (all NaN, or past the end)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          add((v[q] << 1) & 0x1fffcu, 1u << ((v[q] << 4) & 16u), note);
-          add((v[q] >> 15) & 0x1fffcu, 1u << ((v[q] >> 12) & 16u), note);
+          const uint32_t w = counted(v[q]);
+          add((w << 1) & 0x1fffcu, 1u << ((w << 4) & 16u), note);
+          add((w >> 15) & 0x1fffcu, 1u << ((w >> 12) & 16u), note);
         }
       }
     };
@@ -839,11 +845,15 @@ __global__ void __launch_bounds__(NT) sample_bf16_kernel(SampleArgs a) {
         add_all(j, v);
       });
     else visit<false>(s, 0, lane, add_all);
-    if (s.extra >= 0) add((xbits >> 15) & 0x1fffcu, 1u << ((xbits >> 12) & 16u), note);
+    if (s.extra >= 0) {
+      const uint32_t w = counted(xbits);
+      add((w >> 15) & 0x1fffcu, 1u << ((w >> 12) & 16u), note);
+    }
     __syncthreads();
     // The sum of all counts, and which steps have any (a wave reads the words of
-    // one step at a time).  (-inf and the odd pattern beside it, a NaN, are never
-    // kept: their word counts as one number, so masking with -inf wraps nothing.)
+    // one step at a time).  (The odd pattern beside -inf, a NaN, is counted as -inf:
+    // their word is one number, so masking with -inf wraps nothing.  Every count that
+    // wraps lowers the sum and nothing raises it, so it is V only if none did.)
     uint32_t sum = 0;
 #pragma unroll 8
     for (int i = 0; i < 32768 / NT; ++i) {

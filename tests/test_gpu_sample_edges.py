@@ -83,3 +83,24 @@ def test_counts_of_negative_zeros_past_16_bits(V, n):
     x, u = x.bfloat16(), torch.rand(2, generator=g)
     run(x, u)
     run(x, u, 1.0, 0, 0.3)
+
+
+def patterns(*parts):
+    """A bf16 row of the given (16-bit pattern, count) parts."""
+    bits = torch.cat([torch.full((n,), p - 65536 if p > 32767 else p, dtype=torch.int16) for p, n in parts])
+    return bits.view(torch.bfloat16)
+
+
+@pytest.mark.parametrize("nan,count", [(0xff81, 1), (0xff81, 2), (0xff81, 70000), (0xffff, 9), (0x7f81, 1), (0xffc0, 65537)])
+@pytest.mark.parametrize("equal", [0x3f80, 0x3f81, 0x8000, 0xff80])
+def test_counts_past_16_bits_beside_nan(nan, count, equal):
+    """NaN of any payload is never kept, and hides no count that wraps: 70000 and 140000
+    equal entries beside it, in the order of their patterns and in any."""
+    g = torch.Generator().manual_seed(equal + count)
+    for n in (70000, 140000):
+        row = patterns((equal, n), (nan, count), (0xbf80, 3000), (0x3f00, 7))
+        x = torch.stack([row, row[torch.randperm(len(row), generator=g)]] * 2)
+        u = torch.tensor([0.0, 0.5, 0.25, 0.9999])
+        run(x, u)
+        run(x, u, 0.5, 0, 0.9)
+        run(x, u, 1.0, 2000, 0.9)
