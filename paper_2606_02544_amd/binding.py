@@ -716,9 +716,24 @@ def _vector(name: str, t, n: int, dtype, device):
         _tensor(name, t, (n,), dtype, device)
 
 
+def _in_32_bits(name: str, x: int) -> int:
+    if not -2 ** 31 <= x < 2 ** 31:
+        _raise(f"{name} = {x} does not fit 32 bits")
+    return x
+
+
+def _filled(kind, fields):
+    """A descriptor of these values.  ctypes drops the upper bits of an integer that
+    its field does not hold: such a value would be taken for another one."""
+    for (name, field), x in zip(kind._fields_, fields):
+        if field is ctypes.c_int32:
+            _in_32_bits(name, x)
+    return kind(*fields)
+
+
 @functools.lru_cache(maxsize=1024)
 def _rotary_desc(*fields) -> RotaryDesc:
-    return RotaryDesc(*fields)
+    return _filled(RotaryDesc, fields)
 
 
 def _rotary_parts(q, k, freq):
@@ -744,11 +759,12 @@ def rope_frequencies(rotary_dim: int, theta: float, *, scaling: str = "none", fa
     kinds = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
     if scaling not in kinds:
         _raise(f"scaling must be one of {sorted(kinds)}, got {scaling!r}")
-    n = operator.index(rotary_dim)
+    n = _in_32_bits("rotary_dim", operator.index(rotary_dim))
+    context = _in_32_bits("original_context", operator.index(original_context))
     freq = torch.empty(max(n, 2) // 2, dtype=torch.float64)
     attn_factor = ctypes.c_float()
     _check(lib().simsd_rope_frequencies(
-        n, theta, kinds[scaling], factor, operator.index(original_context), beta_fast, beta_slow,
+        n, theta, kinds[scaling], factor, context, beta_fast, beta_slow,
         ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double)), ctypes.byref(attn_factor)))
     return freq.to(device), attn_factor.value
 
@@ -878,7 +894,7 @@ def chunk_workspace_size(desc: ChunkDesc) -> int:
 def _chunk_desc(device: torch.device, *fields):
     """ChunkDesc of these field values (read only: calls share it) and the
     workspace bytes of its call on `device`, which is current."""
-    desc = ChunkDesc(*fields)
+    desc = _filled(ChunkDesc, fields)
     return desc, chunk_workspace_size(desc)
 
 
@@ -938,7 +954,7 @@ def chunk_attention(q, k_cache, v_cache, block_table, q_starts, kv_lens, *, max_
 
 @functools.lru_cache(maxsize=1024)
 def _sample_desc(*fields) -> SampleDesc:
-    return SampleDesc(*fields)
+    return _filled(SampleDesc, fields)
 
 
 def sample(logits, uniforms, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None,
