@@ -895,6 +895,8 @@ def _chunk_desc(device: torch.device, *fields):
     """ChunkDesc of these field values (read only: calls share it) and the
     workspace bytes of its call on `device`, which is current."""
     desc = _filled(ChunkDesc, fields)
+    if desc.scale == 0.0 and fields[-2] != 0.0:
+        _raise(f"scale = {fields[-2]} is 0 in fp32, which stands for 1/sqrt(head_dim)")
     return desc, chunk_workspace_size(desc)
 
 

@@ -1,5 +1,5 @@
-"""Whole numbers that do not fit a descriptor's 32-bit fields are refused by the
-operators' entry points (CPU; nothing is launched)."""
+"""Numbers that a descriptor's 32-bit fields cannot hold are refused by the operators'
+entry points (CPU; nothing is launched)."""
 
 import contextlib
 import types
@@ -56,3 +56,11 @@ def test_frequencies(x):
         binding.rope_frequencies(64, 10000.0, scaling="yarn", factor=2.0, original_context=x, device="cpu")
     with pytest.raises(ValueError, match="rotary_dim"):
         binding.rope_frequencies(x, 10000.0, device="cpu")
+
+
+@pytest.mark.parametrize("scale", [1e-46, -1e-50, 5e-324])
+def test_scale_that_vanishes(scale):
+    """(0 stands for the default.)"""
+    with pytest.raises(ValueError, match="scale"):
+        binding.chunk_attention(z(6, 4, 64), z(2, 20, 2, 64), z(2, 20, 2, 64), None, z(3, dtype=I32), z(2, dtype=I32),
+                                max_q_len=6, max_kv_len=20, scale=scale)
