@@ -537,8 +537,10 @@ typedef struct {
  * Logits of -inf or NaN, and those more than 700 T below m, are never kept.
  * If m is +inf, only the logits of +inf are.  T <= 0 (or NaN) selects the first
  * token of the order.  A row that keeps nothing gives token -1.  The random
- * numbers are the caller's, and the running sums are exact to 1e-8 of the
- * largest weight and the same on every run.
+ * numbers are the caller's, and the running sums are the same on every run and
+ * exact to V * 2^-(63 - ceil(log2 V)) of the largest weight (weights are rounded
+ * to as many binary places as V of them leave in 62 bits): 7.5e-9 at most up to
+ * V = 2^18, 1.2e-7 at 2^20, 1.9e-6 at 2^22.
  *
  *   logits       [rows, V], aligned to their elements
  *   uniforms     [rows] float32 in [0, 1)

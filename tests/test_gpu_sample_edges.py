@@ -104,3 +104,20 @@ def test_counts_past_16_bits_beside_nan(nan, count, equal):
         run(x, u)
         run(x, u, 0.5, 0, 0.9)
         run(x, u, 1.0, 2000, 0.9)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [2 ** 18, 2 ** 20 - 3, 2 ** 22])
+def test_sums_of_long_vocabularies(dtype, V):
+    """A tail of equal tokens whose weights, near an odd number of half units, are all
+    rounded one way: in fp32 the sums are off by nearly as much as they may be (2e-6 of
+    the largest weight at 2^22)."""
+    unit = 2.0 ** -(62 - (V - 1).bit_length())
+    x = torch.empty((4, V))
+    for i, w in enumerate((0.45, 0.55, 1.45, 2.55)):
+        x[i] = float(np.log(w * unit))
+    x[:, V // 2] = 0.0
+    x = x.to(DT[dtype])
+    u = torch.tensor([0.0, 0.5, 0.25, 0.75])
+    run(x, u)
+    run(x, u, 1.0, 0, 0.5)
