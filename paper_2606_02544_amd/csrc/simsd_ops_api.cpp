@@ -17,6 +17,15 @@ static simsd_status hip_fail(hipError_t e, const char* what) {
   return SIMSD_ERR_HIP;
 }
 
+// What an entry returns where an exception ends it (no memory for a message, say).
+static simsd_status internal_error(const char* what) noexcept {
+  try {
+    set_error(std::string(what) + ": internal error");
+  } catch (...) {
+  }
+  return SIMSD_ERR_HIP;
+}
+
 static RotaryArgs rotary_args(const simsd_rotary_desc* d, const RotaryPlan& p) {
   RotaryArgs a{};
   a.tokens = d->num_tokens;
@@ -71,8 +80,7 @@ extern "C" simsd_status simsd_rotary(const simsd_rotary_desc* desc, const void* 
     if (e != hipSuccess) return hip_fail(e, "simsd_rotary launch");
     return SIMSD_OK;
   } catch (...) {
-    set_error("simsd_rotary: internal error");
-    return SIMSD_ERR_HIP;
+    return internal_error("simsd_rotary");
   }
 }
 
@@ -108,15 +116,17 @@ extern "C" simsd_status simsd_rotary_append(const simsd_rotary_desc* desc, const
     if (e != hipSuccess) return hip_fail(e, "simsd_rotary_append launch");
     return SIMSD_OK;
   } catch (...) {
-    set_error("simsd_rotary_append: internal error");
-    return SIMSD_ERR_HIP;
+    return internal_error("simsd_rotary_append");
   }
 }
 
 extern "C" size_t simsd_chunk_attention_workspace_size(const simsd_chunk_desc* desc) {
-  ChunkPlan p;
-  if (plan_chunk(desc, current_cus(), &p) != SIMSD_OK) return 0;
-  return p.workspace;
+  try {
+    ChunkPlan p;
+    return plan_chunk(desc, current_cus(), &p) == SIMSD_OK ? p.workspace : 0;
+  } catch (...) {
+    return 0;
+  }
 }
 
 extern "C" simsd_status simsd_chunk_attention(const simsd_chunk_desc* desc, const void* q,
@@ -169,8 +179,7 @@ extern "C" simsd_status simsd_chunk_attention(const simsd_chunk_desc* desc, cons
     if (e != hipSuccess) return hip_fail(e, "simsd_chunk_attention launch");
     return SIMSD_OK;
   } catch (...) {
-    set_error("simsd_chunk_attention: internal error");
-    return SIMSD_ERR_HIP;
+    return internal_error("simsd_chunk_attention");
   }
 }
 
@@ -202,7 +211,6 @@ extern "C" simsd_status simsd_sample(const simsd_sample_desc* desc, const void* 
     if (e != hipSuccess) return hip_fail(e, "simsd_sample launch");
     return SIMSD_OK;
   } catch (...) {
-    set_error("simsd_sample: internal error");
-    return SIMSD_ERR_HIP;
+    return internal_error("simsd_sample");
   }
 }

@@ -348,10 +348,9 @@ simsd_status check_sample_args(const simsd_sample_desc* d, const void* logits, c
 
 using namespace simsd;
 
-extern "C" simsd_status simsd_rope_frequencies(int32_t rotary_dim, double theta,
-                                               simsd_rope_scaling scaling, double factor,
-                                               int32_t original_context, double beta_fast,
-                                               double beta_slow, double* freq, float* attn_factor) {
+static simsd_status rope_frequencies(int32_t rotary_dim, double theta, const simsd_rope_scaling& scaling,
+                                     double factor, int32_t original_context, double beta_fast,
+                                     double beta_slow, double* freq, float* attn_factor) {
   int kind;
   std::memcpy(&kind, &scaling, sizeof kind);
   if (!freq || !attn_factor) return fail(SIMSD_ERR_NULL_POINTER, "rope_frequencies: NULL output");
@@ -395,4 +394,16 @@ extern "C" simsd_status simsd_rope_frequencies(int32_t rotary_dim, double theta,
     }
   }
   return SIMSD_OK;
+}
+
+extern "C" simsd_status simsd_rope_frequencies(int32_t rotary_dim, double theta,
+                                               simsd_rope_scaling scaling, double factor,
+                                               int32_t original_context, double beta_fast,
+                                               double beta_slow, double* freq, float* attn_factor) {
+  try {
+    return rope_frequencies(rotary_dim, theta, scaling, factor, original_context, beta_fast, beta_slow, freq,
+                            attn_factor);
+  } catch (...) {                                // (no memory for the message)
+    return SIMSD_ERR_HIP;
+  }
 }
