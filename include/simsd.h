@@ -489,7 +489,13 @@ size_t simsd_chunk_attention_workspace_size(const simsd_chunk_desc* desc);
  * position p = kv_lens[b] - n_b + i and sees the cached keys
  *   t < min(kv_lens[b], (p / m + 1) * m),   m = mask_block  (all for m = 0),
  * none if p < 0.  A row that sees no key gives 0 and a log-sum-exp of -inf.
- * Keys and values a row does not see have no part in it, whatever they hold.
+ * Keys and values a row does not see have no part in it, whatever they hold.  An
+ * infinite value that it sees makes that element of the row infinite, or NaN where
+ * the key's weight is 0 in fp32 (as 0 times infinity is; which weights round to 0 on
+ * the way may differ with kv_chunk and the shape).  Scores, weights and sums are fp32;
+ * for bf16 the weights are rounded to bf16 for their product with the values, as in
+ * simsd_verify_attention, which adds up to 2^-8 of sum w|v| / sum w to the output's
+ * own rounding.
  *
  *   q           [num_tokens, Hq, head_dim]  (rotated)
  *   k_cache, v_cache, block_table           the cache, as in simsd_attn_desc
