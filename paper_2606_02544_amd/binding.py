@@ -725,9 +725,10 @@ def _in_32_bits(name: str, x: int) -> int:
 def _filled(kind, fields):
     """A descriptor of these values.  ctypes drops the upper bits of an integer that
     its field does not hold: such a value would be taken for another one."""
-    for (name, field), x in zip(kind._fields_, fields):
-        if field is ctypes.c_int32:
-            _in_32_bits(name, x)
+    if not (min(fields) >= -2 ** 31 and max(fields) < 2 ** 31):   # (a wide stride, a NaN or a number too large)
+        for (name, field), x in zip(kind._fields_, fields):
+            if field is ctypes.c_int32:
+                _in_32_bits(name, x)
     return kind(*fields)
 
 
