@@ -508,6 +508,8 @@ size_t simsd_chunk_attention_workspace_size(const simsd_chunk_desc* desc);
  * one work-group takes all keys of a row; a call with less returns
  * SIMSD_ERR_WORKSPACE).  One kernel, and a second that joins the parts of rows
  * whose keys were divided.  The order of additions is fixed for a given shape.
+ * A call of more row blocks (16 to 256 rows of Hq / Hkv to a token) times KV heads
+ * than 2^22, or of more than 65535 key ranges, returns SIMSD_ERR_BAD_SHAPE.
  */
 simsd_status simsd_chunk_attention(const simsd_chunk_desc* desc, const void* q, const void* k_cache,
                                    const void* v_cache, const int32_t* block_table,

@@ -116,6 +116,10 @@ __device__ inline bool setup_block(const ChunkArgs& a, Block& w) {
   return true;
 }
 
+// Log-sum-exp of a row from its maximum (log2 units) and sum.  (The hardware's
+// logarithm: 2^-22 off, what an fp32 log-sum-exp of 4 or more is rounded by anyway.)
+__device__ inline float log_sum(float m, float l) { return (m + __log2f(l)) * kLn2; }
+
 // Partials: O[split][token][head][D] fp32, then (max, sum)[split][token][head].
 __device__ inline int64_t partial_row(const ChunkArgs& a, int split, int token, int head) {
   return (static_cast<int64_t>(split) * a.tokens + token) * a.hq + head;
@@ -449,6 +453,8 @@ __global__ void __launch_bounds__(RW * KW * 64, 2) chunk_bf16_kernel(ChunkArgs a
 
       // O^T += V^T P^T, two 16-key chunks per block.  Chunk hf of block kb
       // covers keys 32*kb + 16*hf + kappa(h, i), kappa(h, i) = 8*(i/4) + 4*h + i%4.
+      // (The weights go in as bf16, the type of the other operand: half a step, 2^-8
+      // of each at most, as the output's own rounding is.  l_run adds them up in fp32.)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         u32x4 pw;
@@ -556,7 +562,7 @@ __global__ void __launch_bounds__(RW * KW * 64, 2) chunk_bf16_kernel(ChunkArgs a
           *reinterpret_cast<u32x2*>(orow + 32 * c + 8 * q + 4 * h) = v;
         }
       if (a.lse && h == 0)
-        a.lse[static_cast<int64_t>(hq) * a.tokens + token] = limit > 0 ? (m_run + __log2f(l_tot)) * kLn2 : kNegInf;
+        a.lse[static_cast<int64_t>(hq) * a.tokens + token] = limit > 0 ? log_sum(m_run, l_tot) : kNegInf;
     } else {
       const int64_t r = partial_row(a, w.split, token, hq);
       float* part = a.part + r * D;
@@ -582,8 +588,9 @@ __global__ void __launch_bounds__(RW * KW * 64, 2) chunk_bf16_kernel(ChunkArgs a
 //   O^T += V^T P^T: MFMA j contracts keys 4 {0..3} + j.  Register j of the
 //     scores is key 4 q + j of row n already; the V^T operand is key 4 q + j, dim
 //     64 u + 4 n + e, register e of the 16-byte load (j, u).
-// It serves few rows (8 single tokens over up to 4000 keys, 32/8 heads: 36 us; a prompt of
-// 512: 36 us, of 1000: 118, where the kernel below takes 103).
+// It serves few rows (single tokens over 4000 keys, 32/8 heads: 8 of them 51 us, 5.2 TB/s,
+// 64 of them 364 us, 5.8 TB/s; a prompt of 512: 36 us, of 1000: 118, where the kernel below
+// takes 103).
 // ----------------------------------------------------------------------------
 template <int D, int RB, bool PAGED>
 __global__ void __launch_bounds__(256, 2) chunk_f32_kernel(ChunkArgs a) {
@@ -826,7 +833,7 @@ __global__ void __launch_bounds__(256, 2) chunk_f32_kernel(ChunkArgs a) {
       const float inv = valid ? 1.f / l : 0.f;
       *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + (static_cast<int64_t>(token) * a.hq + hq) * D + d0) = acc * inv;
       if (a.lse && d0 == 0)
-        a.lse[static_cast<int64_t>(hq) * a.tokens + token] = valid ? (mt + __log2f(l)) * kLn2 : kNegInf;
+        a.lse[static_cast<int64_t>(hq) * a.tokens + token] = valid ? log_sum(mt, l) : kNegInf;
     } else {
       const int64_t r = partial_row(a, w.split, token, hq);
       *reinterpret_cast<f32x4*>(a.part + r * D + d0) = acc;
@@ -1070,7 +1077,7 @@ __global__ void __launch_bounds__(256, 2) chunk_f32_rows_kernel(ChunkArgs a) {
             f32x4{o[r][4 * u][i], o[r][4 * u + 1][i], o[r][4 * u + 2][i], o[r][4 * u + 3][i]} * by;
     if (q == 0) {
       if (!whole) a.part_ml[at] = float2{m_run[r], l};
-      else if (a.lse) a.lse[static_cast<int64_t>(hq) * a.tokens + token] = limit[r] > 0 ? (m_run[r] + __log2f(l)) * kLn2 : kNegInf;
+      else if (a.lse) a.lse[static_cast<int64_t>(hq) * a.tokens + token] = limit[r] > 0 ? log_sum(m_run[r], l) : kNegInf;
     }
   }
 }
@@ -1154,7 +1161,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a) {
   else
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = o * inv;
   if (a.lse && d0 == 0)
-    a.lse[static_cast<int64_t>(head) * a.tokens + token] = limit > 0 ? (m + __log2f(l)) * kLn2 : kNegInf;
+    a.lse[static_cast<int64_t>(head) * a.tokens + token] = limit > 0 ? log_sum(m, l) : kNegInf;
 }
 
 template <int D, bool PAGED>

@@ -23,16 +23,17 @@
 // row is read again), is read from memory once, and the weights are taken of the
 // distinct values only (some 3000 of a row of 151936 logits N(0, 4)).  A counter that
 // passes 65535 shows in the total and the histogram is built again, noting each wrap.
-// What bounds a row is one work-group's LDS and issue, not memory: of the 33 us of a
-// row of 151936, 3 are the read, 15 the counting (2432 LDS atomics of a wave, 15
-// cycles each), 5 the weights, the rest the cuts and the token's index.
+// What bounds a row is one work-group's LDS and issue, not memory: of a row of 151936
+// (4 rows N(0, 4) without a filter: 42 us; 256: 52; 512: 95), a tenth is the read, nearly
+// half the counting (2432 LDS atomics of a wave, 15 cycles each), a sixth the weights, the
+// rest the cuts and the token's index.
 // fp32 rows: the weights are added up in 8192 bins of the upper 13 bits of the
 // ordered bit pattern; a search goes on in the bin it ends in, 10 and then 9
 // bits further, over the row again, which the caches hold by then.
 // What bounds them: two LDS atomics and an fp64 exp an entry, in one work-group a row (4
-// rows of 151936: 169 us without a filter, 225 with top-p; 256 rows: 212 and 281).  A
-// list of the bin's entries for the last 9 bits made rows with k = 1000 faster (233 -> 197)
-// and others, whose bins hold more than it, slower (281 -> 304).
+// rows of 151936: 156 us without a filter, 229 with top-p; 256 rows: 210 and 271).  A
+// list of the bin's entries for the last 9 bits made rows with k = 1000 faster (by 15 %)
+// and others, whose bins hold more than it, slower (by 8 %).
 #include <type_traits>
 
 #include "simsd_ops_kernels.h"
