@@ -12,6 +12,7 @@ import ctypes
 import functools
 import operator
 import os
+import threading
 from typing import Optional
 
 import torch
@@ -887,6 +888,12 @@ def rotary_append(q, k, v, k_cache, v_cache, block_table, q_starts, kv_lens, fre
     return q_out
 
 
+# Host threads that call on one stream share its buffer: the two kernels of a call are
+# enqueued with no other call's between them.  (A ctypes call releases the interpreter's
+# own lock.)
+_chunk_order = threading.Lock()
+
+
 def chunk_workspace_size(desc: ChunkDesc) -> int:
     return int(lib().simsd_chunk_attention_workspace_size(ctypes.byref(desc)))
 
@@ -948,10 +955,11 @@ def chunk_attention(q, k_cache, v_cache, block_table, q_starts, kv_lens, *, max_
                 workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
             else:
                 workspace = WORKSPACES.get(dev, at.handle, "chunk", nbytes)
-        _check(lib().simsd_chunk_attention(
-            ctypes.byref(desc), q.data_ptr(), _addr(k_cache), _addr(v_cache),
-            _addr(block_table if pages else None), q_starts.data_ptr(), kv_lens.data_ptr(),
-            out.data_ptr(), _addr(lse), _addr(workspace), _nbytes(workspace), at.handle))
+        with _chunk_order:
+            _check(lib().simsd_chunk_attention(
+                ctypes.byref(desc), q.data_ptr(), _addr(k_cache), _addr(v_cache),
+                _addr(block_table if pages else None), q_starts.data_ptr(), kv_lens.data_ptr(),
+                out.data_ptr(), _addr(lse), _addr(workspace), _nbytes(workspace), at.handle))
     return out, lse
 
 

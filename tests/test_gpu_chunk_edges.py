@@ -57,3 +57,30 @@ def test_with_weights_that_vanish(dtype, max_q, kv_chunk):
     hit = out.cpu()[sees]
     assert bool((hit.isnan() | (hit == INF)).all())
     assert torch.equal(out.cpu()[~sees], base.cpu()[~sees]) and torch.equal(lse, base_lse)
+
+
+def test_threads_that_share_a_stream():
+    """Calls with key ranges from several host threads on the default stream."""
+    import threading
+    from paper_2606_02544_amd import binding
+    sets = [make([(2, 900), (1, 700)], 8, 2, 128, "bf16", 16, 50 + i) for i in range(3)]
+    dev = [[s[n].cuda() for n in ("q", "k", "v", "table", "starts", "kv")] for s in sets]
+    one = lambda i: binding.chunk_attention(*dev[i], max_q_len=2, max_kv_len=sets[i]["cap"], page_size=16,  # noqa: E731
+                                            kv_chunk=64)
+    want = [one(i) for i in range(3)]
+    got = [[], [], []]
+
+    def thread(i):
+        for _ in range(40):
+            got[i].append(one(i))
+
+    threads = [threading.Thread(target=thread, args=(i,)) for i in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(3):
+        assert len(got[i]) == 40
+        for out, lse in got[i]:
+            assert torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1])
