@@ -29,6 +29,13 @@
  *                           tokens over that cache (no drafts);
  *   simsd_sample            one token a row from filtered logits: what the drafter
  *                           proposes, or the target where nothing was drafted.
+ * and, for long contexts in bounded memory:
+ *   simsd_chunk_attention_window, simsd_verify_attention_window
+ *                           both attentions under a sliding window whose first
+ *                           tokens (sinks) stay visible;
+ *   simsd_rotary_append_fp4, simsd_chunk_attention_fp4,
+ *   simsd_verify_attention_fp4, simsd_fp4_values
+ *                           a cache held in 4 bits: filled, attended over, read back.
  *
  * Conventions shared by all calls
  * --------------------------------
@@ -516,6 +523,140 @@ simsd_status simsd_chunk_attention(const simsd_chunk_desc* desc, const void* q, 
                                    const int32_t* q_starts, const int32_t* kv_lens, void* out,
                                    float* lse, void* workspace, size_t workspace_bytes,
                                    void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Sliding window with sinks                                                  */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * simsd_chunk_attention for layers whose tokens see a window of the latest keys and
+ * a few first ones.  A token at position p, in the mask's block of m = mask_block
+ * positions that starts at p0 = p / m * m, sees the cached keys
+ *   t < min(kv_lens[b], p0 + m)  with  t > p0 - window  or  t < sinks:
+ * its own block as before (m = 1: itself), the window - 1 keys before that, and the
+ * first `sinks` keys.  All tokens of a block see the same keys.
+ *
+ *   window  >= 1, or 0: none (then sinks must be 0 too)
+ *   sinks   >= 0
+ * A window needs mask_block >= 1 (SIMSD_ERR_BAD_SHAPE otherwise).  Everything else is
+ * as in simsd_chunk_attention, with its own workspace size; kv_chunk counts the keys
+ * of the tiles of 64 that a row block's window and sinks lie in (fp32: 32).  Pages
+ * none of whose keys a token of the call sees are not read, and neither are their
+ * entries of block_table: both may have been given to other sequences.
+ */
+size_t simsd_chunk_attention_window_workspace_size(const simsd_chunk_desc* desc, int32_t window,
+                                                   int32_t sinks);
+simsd_status simsd_chunk_attention_window(const simsd_chunk_desc* desc, int32_t window, int32_t sinks,
+                                          const void* q, const void* k_cache, const void* v_cache,
+                                          const int32_t* block_table, const int32_t* q_starts,
+                                          const int32_t* kv_lens, void* out, float* lse,
+                                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * simsd_verify_attention under the same window: the new slots are the block that
+ * starts at position prefix_lens[b], so that each of them sees the cached keys
+ *   t > prefix_lens[b] - window  or  t < sinks,
+ * and the new slots that the temporal mask allows.  window 0: the whole prefix.
+ * SIMSD_ERR_UNSUPPORTED: fp32, rope_theta > 0 (turn q and k_new with simsd_rotary),
+ * kv_chunk < 0.  kv_chunk counts as in simsd_chunk_attention_window, the tile of the
+ * new slots among them.  Keys and values a slot does not see have no part in its
+ * row, whatever they hold.
+ */
+size_t simsd_verify_attention_window_workspace_size(const simsd_attn_desc* desc, int32_t window,
+                                                    int32_t sinks);
+simsd_status simsd_verify_attention_window(const simsd_attn_desc* desc, int32_t window, int32_t sinks,
+                                           const void* q, const void* k_new, const void* v_new,
+                                           const void* k_cache, const void* v_cache,
+                                           const int32_t* block_table, const int32_t* prefix_lens,
+                                           const int32_t* step_map, const int32_t* num_ref, void* out,
+                                           float* lse, void* workspace, size_t workspace_bytes,
+                                           void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* A cache held in 4 bits                                                     */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Keys and values in 4.25 bits an element.  32 dims of a head, from a multiple of 32
+ * on, share a power of two 2^e; each is a code c of 4 bits: its sign, and the index of
+ * its size in {0, 0.5, 1, 1.5, 2, 3, 4, 6}, times 2^e.
+ *   codes   head_dim / 2 bytes a head, dims 2i and 2i + 1 in the low and high half of
+ *           byte i
+ *   scales  head_dim / 32 bytes a head, e + 127 each; 255: all 32 are NaN
+ * Codes lie like the elements of a cache (see simsd_attn_desc), with the descriptor's
+ * cache strides in bytes; scales with strides of their own.  A cache of zeros holds
+ * zeros.  What a head's tokens take is least fetched where they lie next to each other
+ * (strides of head outside token).
+ */
+typedef struct {
+  void* k;                    /* codes, 16-byte aligned                           */
+  void* v;
+  void* k_scales;             /* scales, no alignment                             */
+  void* v_scales;
+  int64_t scale_stride_seq;   /* bytes between sequences (contiguous) / pages     */
+  int64_t scale_stride_token;
+  int64_t scale_stride_head;
+} simsd_fp4_cache;
+
+/*
+ * simsd_rotary_append to a 4-bit cache.  A turned key is rounded once, from the exact
+ * rotation (1e-15) to the nearest code, ties to the even one; values likewise as they
+ * are.  e is the least exponent, from -125 to 125, at which the largest of the 32 is
+ * below 7 * 2^e (it is held as 6 * 2^e at most); larger ones than 6 * 2^125 are held
+ * as that.  32 of which one is infinite or NaN are all held as NaN.  Queries are
+ * turned as in simsd_rotary_append.
+ *   dtype SIMSD_BF16 and head_dim 64 or 128 only (SIMSD_ERR_UNSUPPORTED); cache
+ *   strides in bytes, those of the codes multiples of 16; tokens' and heads' rows of
+ *   codes and of scales apart.
+ */
+simsd_status simsd_rotary_append_fp4(const simsd_rotary_desc* desc, const void* q, const void* k,
+                                     const void* v, const int32_t* positions, const double* freq,
+                                     void* q_out, const simsd_fp4_cache* cache,
+                                     const int32_t* block_table, const int32_t* q_starts,
+                                     const int32_t* kv_lens, void* stream);
+
+/*
+ * simsd_chunk_attention_window over a 4-bit cache: its keys and values are the exact
+ * values of their codes, and the arithmetic is that of bf16.  dtype (of q and out)
+ * SIMSD_BF16 only (SIMSD_ERR_UNSUPPORTED); cache_stride_* in bytes, multiples of 16.
+ */
+size_t simsd_chunk_attention_fp4_workspace_size(const simsd_chunk_desc* desc, int32_t window,
+                                                int32_t sinks);
+simsd_status simsd_chunk_attention_fp4(const simsd_chunk_desc* desc, int32_t window, int32_t sinks,
+                                       const void* q, const simsd_fp4_cache* cache,
+                                       const int32_t* block_table, const int32_t* q_starts,
+                                       const int32_t* kv_lens, void* out, float* lse, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
+ * simsd_verify_attention_window over a 4-bit prefix (k_new and v_new in bf16; the
+ * accepted ones are appended with simsd_rotary_append_fp4).
+ */
+size_t simsd_verify_attention_fp4_workspace_size(const simsd_attn_desc* desc, int32_t window,
+                                                 int32_t sinks);
+simsd_status simsd_verify_attention_fp4(const simsd_attn_desc* desc, int32_t window, int32_t sinks,
+                                        const void* q, const void* k_new, const void* v_new,
+                                        const simsd_fp4_cache* cache, const int32_t* block_table,
+                                        const int32_t* prefix_lens, const int32_t* step_map,
+                                        const int32_t* num_ref, void* out, float* lse,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Codes [n0, n1, n2, head_dim / 2] and scales [n0, n1, n2, head_dim / 32] of a cache's
+ * keys or values, with strides in bytes. */
+typedef struct {
+  int64_t n0;                 /* sequences or pages, 0..2^31 - 1                  */
+  int32_t n1, n2;             /* tokens and heads, >= 0; n0 * n1 * n2 <= 2^36     */
+  int32_t head_dim;           /* a multiple of 32, 32..512                        */
+  int64_t code_stride[3];     /* multiples of 4                                   */
+  int64_t scale_stride[3];
+} simsd_fp4_values_desc;
+
+/*
+ * out [n0, n1, n2, head_dim] bf16, 16-byte aligned: the codes' values.  Exact; past
+ * bf16's range infinite (no append writes such).  codes 4-byte aligned.  One kernel.
+ */
+simsd_status simsd_fp4_values(const simsd_fp4_values_desc* desc, const void* codes,
+                              const void* scales, void* out, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Sampling                                                                   */

@@ -20,6 +20,8 @@ A plain, slow, float64 numpy statement of what the GPU path computes:
   * ``rotary``    rotary positions in every layout, scaled frequencies, and the
                   cache rows that a ragged batch's new tokens take;
   * ``chunk``     softmax attention of new tokens under the block-causal mask;
+  * ``window``    the same, and the verification's, under a sliding window with sinks;
+  * ``fp4``       the cache's 4-bit form, encoded and decoded;
   * ``sampling``  temperature, top-k, top-p and min-p over a sorted row, and the
                   draw from a given uniform number.
 

@@ -13,7 +13,7 @@ import functools
 import operator
 import os
 import threading
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -76,6 +76,18 @@ class SampleDesc(ctypes.Structure):
                 ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("dtype", ctypes.c_int)]
 
 
+class Fp4Pointers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales")] + \
+               [(n, ctypes.c_int64) for n in
+                ("scale_stride_seq", "scale_stride_token", "scale_stride_head")]
+
+
+class Fp4ValuesDesc(ctypes.Structure):
+    _fields_ = [("n0", ctypes.c_int64), ("n1", ctypes.c_int32), ("n2", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("code_stride", ctypes.c_int64 * 3),
+                ("scale_stride", ctypes.c_int64 * 3)]
+
+
 class SimsdError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -132,6 +144,28 @@ def lib() -> ctypes.CDLL:
         L.simsd_chunk_attention.restype = ctypes.c_int
         L.simsd_sample.argtypes = [ctypes.POINTER(SampleDesc)] + [_P] * 10
         L.simsd_sample.restype = ctypes.c_int
+        for kind, desc in (("chunk", ChunkDesc), ("verify", AttnDesc)):
+            for form in ("window", "fp4"):
+                size = getattr(L, f"simsd_{kind}_attention_{form}_workspace_size")
+                size.argtypes = [ctypes.POINTER(desc), ctypes.c_int32, ctypes.c_int32]
+                size.restype = ctypes.c_size_t
+        head = [ctypes.POINTER(ChunkDesc), ctypes.c_int32, ctypes.c_int32, _P]
+        tail = [_P] * 6 + [ctypes.c_size_t, _P]
+        L.simsd_chunk_attention_window.argtypes = head + [_P, _P] + tail
+        L.simsd_chunk_attention_window.restype = ctypes.c_int
+        L.simsd_chunk_attention_fp4.argtypes = head + [ctypes.POINTER(Fp4Pointers)] + tail
+        L.simsd_chunk_attention_fp4.restype = ctypes.c_int
+        head = [ctypes.POINTER(AttnDesc), ctypes.c_int32, ctypes.c_int32, _P, _P, _P]
+        tail = [_P] * 7 + [ctypes.c_size_t, _P]
+        L.simsd_verify_attention_window.argtypes = head + [_P, _P] + tail
+        L.simsd_verify_attention_window.restype = ctypes.c_int
+        L.simsd_verify_attention_fp4.argtypes = head + [ctypes.POINTER(Fp4Pointers)] + tail
+        L.simsd_verify_attention_fp4.restype = ctypes.c_int
+        L.simsd_rotary_append_fp4.argtypes = [ctypes.POINTER(RotaryDesc)] + [_P] * 6 + \
+            [ctypes.POINTER(Fp4Pointers)] + [_P] * 4
+        L.simsd_rotary_append_fp4.restype = ctypes.c_int
+        L.simsd_fp4_values.argtypes = [ctypes.POINTER(Fp4ValuesDesc)] + [_P] * 4
+        L.simsd_fp4_values.restype = ctypes.c_int
         L.simsd_validate_step_map.argtypes = [_I32P, _I32P, ctypes.c_int32, ctypes.c_int32,
                                               ctypes.c_int32]
         L.simsd_validate_step_map.restype = ctypes.c_int
@@ -425,8 +459,9 @@ def verify_attention(q, k_new, v_new, k_cache, v_cache, block_table, prefix_lens
                      rope_theta: float = 0.0,
                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                      want_lse: bool = True, workspace: Optional[torch.Tensor] = None,
-                     stream=None, desc: Optional[AttnDesc] = None):
-    """simsd_verify_attention on torch tensors.  Returns (out, lse).
+                     stream=None, desc: Optional[AttnDesc] = None, window: int = 0, sinks: int = 0):
+    """simsd_verify_attention on torch tensors, or with a window
+    simsd_verify_attention_window (without `desc`).  Returns (out, lse).
 
     Raises ValueError on tensors whose shape, dtype, device or layout does not
     match (before anything is launched), SimsdError if the library rejects
@@ -438,6 +473,15 @@ def verify_attention(q, k_new, v_new, k_cache, v_cache, block_table, prefix_lens
                                       step_map, num_ref, out, lse, block_size=block_size,
                                       max_ref=max_ref, max_prefix_len=max_prefix_len,
                                       page_size=page_size)
+    if window or sinks:
+        if desc is not None:
+            _raise("a window and a descriptor of the caller's do not go together")
+        st = k_cache.stride()[:3] if max_prefix_len > 0 else (0, 0, 0)
+        pages = block_table.shape[1] if max_prefix_len > 0 and page_size > 0 else 0
+        return _verify_span("window", q, k_new, v_new, (_addr(k_cache), _addr(v_cache)), st, pages,
+                            block_table, prefix_lens, step_map, num_ref, hkv, block_size, max_ref,
+                            max_prefix_len, page_size, kv_chunk, scale, rope_theta, window, sinks,
+                            out, lse, want_lse, workspace, stream)
     b, n_new, hq, d = q.shape
     dev = q.device
     if desc is None:
@@ -912,11 +956,14 @@ def chunk_attention(q, k_cache, v_cache, block_table, q_starts, kv_lens, *, max_
                     max_kv_len: int, page_size: int = 0, mask_block: int = 1, kv_chunk: int = 0,
                     scale: float = 0.0, out: Optional[torch.Tensor] = None,
                     lse: Optional[torch.Tensor] = None, want_lse: bool = True,
-                    workspace: Optional[torch.Tensor] = None, stream=None):
+                    workspace: Optional[torch.Tensor] = None, stream=None, window: int = 0,
+                    sinks: int = 0):
     """simsd_chunk_attention on torch tensors: q [tokens, Hq, d], contiguous, the
     new tokens of a ragged batch, over a cache that holds their keys and values.
     Returns (out [tokens, Hq, d], lse [Hq, tokens] or None); rows outside
-    q_starts' range are left as they were.
+    q_starts' range are left as they were.  With a window it is
+    simsd_chunk_attention_window: a token sees its mask's block, the window - 1
+    keys before that and the first `sinks` keys.
 
     Without a caller's workspace a call takes the buffer held for its stream; one
     that is captured into a graph takes memory of that graph's own."""
@@ -937,6 +984,10 @@ def chunk_attention(q, k_cache, v_cache, block_table, q_starts, kv_lens, *, max_
     else:
         hkv = hq
     cs, pages = _cache_strides(k_cache, v_cache, dt, dev, hkv, d, page_size, max_kv_len, b, block_table)
+    if window or sinks:
+        return _chunk_span("window", q, (_addr(k_cache), _addr(v_cache)), cs, pages, block_table, q_starts,
+                           kv_lens, b, hkv, max_q_len, max_kv_len, page_size, mask_block, kv_chunk, scale,
+                           window, sinks, out, lse, want_lse, workspace, stream)
     if out is not None:
         _tensor("out", out, (T, hq, d), dt, dev)
     if lse is not None:
@@ -961,6 +1012,277 @@ def chunk_attention(q, k_cache, v_cache, block_table, q_starts, kv_lens, *, max_
                 _addr(block_table if pages else None), q_starts.data_ptr(), kv_lens.data_ptr(),
                 out.data_ptr(), _addr(lse), _addr(workspace), _nbytes(workspace), at.handle))
     return out, lse
+
+
+# ----------------------------------------------------------------------------
+# A sliding window with sinks, and a cache held in 4 bits
+# ----------------------------------------------------------------------------
+class Fp4Cache(NamedTuple):
+    """Keys and values in 4 bits: codes [seq or page, token, Hkv, d / 2] and scales
+    [seq or page, token, Hkv, d / 32], uint8 (the form is simsd_fp4_cache's)."""
+
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+
+
+def fp4_cache(num: int, tokens: int, num_kv_heads: int, head_dim: int, *, device="cuda") -> Fp4Cache:
+    """A cache of zeros for `num` sequences (or pages) of `tokens` tokens.  A head's
+    tokens lie next to each other, so that a head is read without its neighbours."""
+    if head_dim not in (64, 128):
+        _raise(f"head_dim must be 64 or 128, got {head_dim}")
+
+    def part(width):
+        return torch.zeros((num, num_kv_heads, tokens, width), dtype=torch.uint8, device=device).transpose(1, 2)
+
+    return Fp4Cache(part(head_dim // 2), part(head_dim // 2), part(head_dim // 32), part(head_dim // 32))
+
+
+def _fp4_parts(cache, device, width: int = 0):
+    """Shape of a cache's codes, which with its scales passes the checks here."""
+    if not isinstance(cache, tuple) or len(cache) != 4:
+        _raise("cache must be an Fp4Cache (codes and scales of keys and values)")
+    for name, t in zip(Fp4Cache._fields, cache):
+        if not isinstance(t, torch.Tensor) or t.dim() != 4:
+            _raise(f"cache.{name} must be a 4-D tensor [seq or page, token, Hkv, *]")
+        if t.dtype is not torch.uint8:
+            _raise(f"cache.{name} must be uint8, got {t.dtype}")
+        if t.device != device:
+            _raise(f"cache.{name} is on {t.device}, expected {device}")
+        if t.stride(3) != 1:
+            _raise(f"cache.{name} must have a unit stride over the head dimension")
+    k, v, ks, vs = cache
+    if k.shape != v.shape or k.stride() != v.stride():
+        _raise("shapes or strides of the keys' and values' codes differ")
+    if ks.shape != vs.shape or ks.stride() != vs.stride():
+        _raise("shapes or strides of the keys' and values' scales differ")
+    n, tokens, hkv, half = k.shape
+    if half % 16 or (width and half != width // 2):
+        _raise(f"the codes hold heads of {2 * half} dims" + (f", expected {width}" if width else ": need a multiple of 32"))
+    if ks.shape != (n, tokens, hkv, half // 16):
+        _raise(f"the scales have shape {tuple(ks.shape)}, expected {(n, tokens, hkv, half // 16)}")
+    return k.shape
+
+
+def _fp4_pointers(cache: Fp4Cache):
+    st = cache.k_scales.stride()
+    return Fp4Pointers(cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scales.data_ptr(),
+                       cache.v_scales.data_ptr(), st[0], st[1], st[2])
+
+
+def _fp4_call(cache, device, d, page_size, max_len, batch, block_table):
+    """KV heads, pointers, strides and pages per sequence of a call's 4-bit cache."""
+    if max_len <= 0:
+        return None, Fp4Pointers(), (0, 0, 0), 0
+    n, tokens, hkv, _ = _fp4_parts(cache, device, d)
+    pages = 0
+    if page_size > 0:
+        _need(tokens == page_size, f"paged cache: dimension 1 is {tokens}, page_size is {page_size}")
+        _need(block_table is not None, "paged cache needs a block_table")
+        _int32("block_table", block_table, (batch, None), device)
+        pages = block_table.shape[1]
+        _need(pages * page_size >= max_len, "block_table has too few pages per sequence")
+    else:
+        _need(n == batch, f"contiguous cache: dimension 0 is {n}, batch is {batch}")
+        _need(tokens >= max_len, f"contiguous cache holds {tokens} tokens, need {max_len}")
+    return hkv, _fp4_pointers(cache), cache.k.stride()[:3], pages
+
+
+@functools.lru_cache(maxsize=1024)
+def _span_desc(kind, form, device: torch.device, window: int, sinks: int, *fields):
+    """Descriptor of these field values (read only: calls share it) and the workspace
+    bytes of its call on `device`, which is current."""
+    desc = _filled(kind, fields)
+    scale = fields[14 if kind is ChunkDesc else 13]
+    if desc.scale == 0.0 and scale != 0.0:
+        _raise(f"scale = {scale} is 0 in fp32, which stands for 1/sqrt(head_dim)")
+    what = "chunk" if kind is ChunkDesc else "verify"
+    size = getattr(lib(), f"simsd_{what}_attention_{form}_workspace_size")
+    return desc, int(size(ctypes.byref(desc), window, sinks))
+
+
+def _span_workspace(workspace, nbytes, device, handle):
+    """The caller's buffer, the one held for the stream, or (captured into a graph)
+    memory of that graph's own."""
+    if workspace is not None:
+        _tensor("workspace", workspace, (None,), None, device)
+        return workspace
+    if not nbytes:
+        return None
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return WORKSPACES.get(device, handle, "span", nbytes)
+
+
+def _window(window, sinks):
+    return (_in_32_bits("window", operator.index(window)), _in_32_bits("sinks", operator.index(sinks)))
+
+
+def _chunk_span(form, q, cache, cs, pages, block_table, q_starts, kv_lens, b, hkv, max_q_len, max_kv_len,
+                page_size, mask_block, kv_chunk, scale, window, sinks, out, lse, want_lse, workspace, stream):
+    """Chunk attention by the entry of this form ("window" or "fp4"); the arguments of
+    chunk_attention are checked, `cache` is what that entry takes for it."""
+    (T, hq, d), dt, dev = q.shape, q.dtype, q.device
+    window, sinks = _window(window, sinks)
+    if out is not None:
+        _tensor("out", out, (T, hq, d), dt, dev)
+    if lse is not None:
+        _tensor("lse", lse, (hq, T), torch.float32, dev)
+    with _Launch(dev, stream) as at:
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None and want_lse:
+            lse = torch.empty((hq, T), dtype=torch.float32, device=dev)
+        desc, nbytes = _span_desc(ChunkDesc, form, dev, window, sinks, T, b, hq, hkv, d, max_q_len,
+                                  max_kv_len, mask_block, page_size, pages, kv_chunk, cs[0], cs[1], cs[2],
+                                  float(scale), _dtype_code(dt))
+        workspace = _span_workspace(workspace, nbytes, dev, at.handle)
+        with _chunk_order:
+            _check(getattr(lib(), f"simsd_chunk_attention_{form}")(
+                ctypes.byref(desc), window, sinks, q.data_ptr(), *cache, _addr(block_table if pages else None),
+                q_starts.data_ptr(), kv_lens.data_ptr(), out.data_ptr(), _addr(lse), _addr(workspace),
+                _nbytes(workspace), at.handle))
+    return out, lse
+
+
+def chunk_attention_fp4(q, cache: Optional[Fp4Cache], block_table, q_starts, kv_lens, *, max_q_len: int,
+                        max_kv_len: int, page_size: int = 0, mask_block: int = 1, kv_chunk: int = 0,
+                        scale: float = 0.0, window: int = 0, sinks: int = 0,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                        want_lse: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """simsd_chunk_attention_fp4 on torch tensors: chunk_attention of bf16 queries over
+    a 4-bit cache.  Returns (out, lse)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        _raise("q must be a 3-D tensor [tokens, Hq, d]")
+    if q.dtype is not torch.bfloat16:
+        _raise(f"q must be bfloat16, got {q.dtype}")
+    if not q.is_contiguous():
+        _raise("q must be contiguous")
+    b = _ragged(q_starts, kv_lens, q.device)
+    max_q_len, max_kv_len, page_size, mask_block, kv_chunk = map(
+        operator.index, (max_q_len, max_kv_len, page_size, mask_block, kv_chunk))
+    hkv, pointers, cs, pages = _fp4_call(cache, q.device, q.shape[2], page_size, max_kv_len, b, block_table)
+    return _chunk_span("fp4", q, (ctypes.byref(pointers),), cs, pages, block_table, q_starts, kv_lens, b,
+                       q.shape[1] if hkv is None else hkv, max_q_len, max_kv_len, page_size, mask_block,
+                       kv_chunk, scale, window, sinks, out, lse, want_lse, workspace, stream)
+
+
+def _verify_span(form, q, k_new, v_new, cache, cs, pages, block_table, prefix_lens, step_map, num_ref, hkv,
+                 block_size, max_ref, max_prefix_len, page_size, kv_chunk, scale, rope_theta, window, sinks,
+                 out, lse, want_lse, workspace, stream):
+    """Verification attention by the entry of this form ("window" or "fp4"); the tensors
+    are checked, `cache` is what that entry takes for it."""
+    (b, n_new, hq, d), dt, dev = q.shape, q.dtype, q.device
+    window, sinks = _window(window, sinks)
+    block_size, max_ref, max_prefix_len, page_size, kv_chunk = map(
+        operator.index, (block_size, max_ref, max_prefix_len, page_size, kv_chunk))
+    with _Launch(dev, stream) as at:
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None and want_lse:
+            lse = torch.empty((b, hq, n_new), dtype=torch.float32, device=dev)
+        desc, nbytes = _span_desc(AttnDesc, form, dev, window, sinks, b, hq, hkv, d, block_size, max_ref,
+                                  max_prefix_len, page_size if max_prefix_len > 0 else 0, pages, kv_chunk,
+                                  cs[0], cs[1], cs[2], float(scale), _dtype_code(dt), float(rope_theta))
+        workspace = _span_workspace(workspace, nbytes, dev, at.handle)
+        with _chunk_order:
+            _check(getattr(lib(), f"simsd_verify_attention_{form}")(
+                ctypes.byref(desc), window, sinks, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), *cache,
+                _addr(block_table if pages else None), prefix_lens.data_ptr(), step_map.data_ptr(),
+                num_ref.data_ptr(), out.data_ptr(), _addr(lse), _addr(workspace), _nbytes(workspace),
+                at.handle))
+    return out, lse
+
+
+def verify_attention_fp4(q, k_new, v_new, cache: Optional[Fp4Cache], block_table, prefix_lens, step_map,
+                         num_ref, *, block_size: int, max_ref: int, max_prefix_len: int, page_size: int = 0,
+                         kv_chunk: int = 0, scale: float = 0.0, window: int = 0, sinks: int = 0,
+                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         want_lse: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """simsd_verify_attention_fp4 on torch tensors: verify_attention over a 4-bit
+    prefix.  Returns (out, lse)."""
+    hkv = check_attention_tensors(q, k_new, v_new, None, None, block_table, prefix_lens, step_map, num_ref,
+                                  out, lse, block_size=block_size, max_ref=max_ref, max_prefix_len=0,
+                                  page_size=page_size)
+    b, _, _, d = q.shape
+    held, pointers, cs, pages = _fp4_call(cache, q.device, d, operator.index(page_size),
+                                          operator.index(max_prefix_len), b, block_table)
+    if held is not None and held != hkv:
+        _raise(f"the cache has {held} KV heads, k_new has {hkv}")
+    return _verify_span("fp4", q, k_new, v_new, (ctypes.byref(pointers),), cs, pages, block_table, prefix_lens,
+                        step_map, num_ref, hkv, block_size, max_ref, max_prefix_len, page_size, kv_chunk, scale,
+                        0.0, window, sinks, out, lse, want_lse, workspace, stream)
+
+
+def rotary_append_fp4(q, k, v, cache: Fp4Cache, block_table, q_starts, kv_lens, freq, *, max_kv_len: int,
+                      page_size: int = 0, positions=None, interleaved: bool = False, attn_factor: float = 1.0,
+                      q_out: Optional[torch.Tensor] = None, stream=None):
+    """simsd_rotary_append_fp4 on torch tensors: rotary_append of bf16 heads to a 4-bit
+    cache.  Returns q_out (None without q)."""
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        _raise("k must be a 3-D tensor [tokens, Hkv, d]")
+    T, d, dt, dev, rot = _rotary_parts(k, None, freq)
+    if dt is not torch.bfloat16:
+        _raise(f"q, k and v must be bfloat16, got {dt}")
+    hkv, hq = k.shape[1], 0
+    qs, qo = (0, 0), (0, 0)
+    if q is not None:
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            _raise("q must be a 3-D tensor [tokens, Hq, d]")
+        hq = q.shape[1]
+        qs = _heads("q", q, (T, hq, d), dt, dev)
+        qo = (hq * d if T > 1 else 0, d if hq > 1 else 0) if q_out is None else \
+            _heads("q_out", q_out, (T, hq, d), dt, dev)
+    elif q_out is not None:
+        _raise("q_out without q")
+    ks, vs = _heads("k", k, (T, hkv, d), dt, dev), _heads("v", v, (T, hkv, d), dt, dev)
+    b = _ragged(q_starts, kv_lens, dev)
+    page_size, max_kv_len = operator.index(page_size), operator.index(max_kv_len)
+    held, pointers, cs, pages = _fp4_call(cache, dev, d, page_size, max_kv_len, b, block_table)
+    if held is not None:
+        if held != hkv:
+            _raise(f"the cache has {held} KV heads, k has {hkv}")
+        if any(n > 1 and st == 0 for t in cache for n, st in zip(t.shape, t.stride())):
+            _raise("the cache must not be an expanded tensor: its rows are written")
+    if positions is not None:
+        _vector("positions", positions, T, torch.int32, dev)
+    with _Launch(dev, stream) as at:
+        if q is not None and q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        desc = _rotary_desc(T, hq, hkv, d, rot, int(bool(interleaved)), b, max_kv_len, page_size, pages,
+                            cache.k.shape[0] if pages else 0, float(attn_factor), qs[0], qs[1],
+                            ks[0], ks[1], vs[0], vs[1], qo[0], qo[1], 0, 0, cs[0], cs[1], cs[2],
+                            _dtype_code(dt))
+        _check(lib().simsd_rotary_append_fp4(
+            ctypes.byref(desc), _addr(q), k.data_ptr(), v.data_ptr(), _addr(positions), freq.data_ptr(),
+            _addr(q_out), ctypes.byref(pointers), _addr(block_table if pages else None),
+            q_starts.data_ptr(), kv_lens.data_ptr(), at.handle))
+    return q_out
+
+
+def fp4_values(cache: Fp4Cache, *, k_out: Optional[torch.Tensor] = None,
+               v_out: Optional[torch.Tensor] = None, stream=None):
+    """simsd_fp4_values of a cache's keys and of its values: (k, v), bf16
+    [seq or page, token, Hkv, d], contiguous."""
+    if not isinstance(cache, tuple) or len(cache) != 4 or not isinstance(cache[0], torch.Tensor):
+        _raise("cache must be an Fp4Cache (codes and scales of keys and values)")
+    dev = cache[0].device
+    n, tokens, hkv, half = _fp4_parts(cache, dev)
+    shape = (n, tokens, hkv, 2 * half)
+    for name, out in (("k_out", k_out), ("v_out", v_out)):
+        if out is not None:
+            _tensor(name, out, shape, torch.bfloat16, dev)
+    with _Launch(dev, stream) as at:
+        results = []
+        for codes, scales, out in ((cache[0], cache[2], k_out), (cache[1], cache[3], v_out)):
+            if out is None:
+                out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+            desc = Fp4ValuesDesc(n, tokens, hkv, 2 * half, codes.stride()[:3], scales.stride()[:3])
+            _check(lib().simsd_fp4_values(ctypes.byref(desc), codes.data_ptr(), scales.data_ptr(),
+                                          out.data_ptr(), at.handle))
+            results.append(out)
+    return tuple(results)
 
 
 @functools.lru_cache(maxsize=1024)

@@ -10,8 +10,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["simsd_attention.hip", "simsd_accept.hip", "simsd_lmhead.hip", "simsd_rotary.hip",
-           "simsd_sample.hip", "simsd_chunk.hip", "simsd_api.cpp", "simsd_ops_api.cpp", "simsd_plan.cpp",
-           "simsd_ops_plan.cpp"]
+           "simsd_sample.hip", "simsd_chunk.hip", "simsd_window.hip", "simsd_fp4.hip", "simsd_chunk_fp4.hip",
+           "simsd_verify_span.hip", "simsd_api.cpp", "simsd_ops_api.cpp", "simsd_span_api.cpp",
+           "simsd_plan.cpp", "simsd_ops_plan.cpp", "simsd_span_plan.cpp"]
 OUT = os.path.join(HERE, "libsimsd.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "simsd_ops_plan.h"
+#include "simsd_span_plan.h"
 
 namespace simsd {
 
@@ -48,6 +49,45 @@ struct ChunkArgs {
 
 hipError_t launch_chunk(const simsd_chunk_desc& d, const ChunkPlan& p, const ChunkArgs& a,
                         hipStream_t stream);
+
+// Attention over the cache under a sliding window with sinks, over a 4-bit cache, and
+// of the verification step's new slots.  `chunk` is a multiple of a tile's keys.
+struct SpanArgs : ChunkArgs {
+  int window, sinks;            // window 0: none
+  const uint8_t* k_scales;      // 4-bit cache
+  const uint8_t* v_scales;
+  int64_t ss_seq, ss_tok, ss_head;
+  const void* k_new;            // verification: kv_lens counts the cached prefix alone
+  const void* v_new;
+  const int32_t* step_map;
+  const int32_t* num_ref;
+  int block, n_new, seq_blocks; // B, B + L, row blocks of a sequence
+};
+
+hipError_t launch_window(const SpanPlan& p, bool bf16, int d, const SpanArgs& a, hipStream_t stream);
+hipError_t launch_fp4(const SpanPlan& p, int d, const SpanArgs& a, hipStream_t stream);
+hipError_t launch_verify_span(const SpanPlan& p, bool fp4, int d, const SpanArgs& a, hipStream_t stream);
+
+struct Fp4Args {
+  const void* codes;            // [n0, n1, n2, d / 2]
+  const uint8_t* scales;        // [n0, n1, n2, d / 32]
+  void* out;
+  int64_t c0, c1, c2, s0, s1, s2;
+  int64_t rows;                 // n0 * n1 * n2
+  int n1, n2, groups;
+};
+hipError_t launch_fp4_values(const Fp4Args& a, int cus, hipStream_t stream);
+
+// The append to a 4-bit cache.  `r` is the append of the queries alone (no KV heads), with
+// the keys and values and, in k_out and v_out, the cache's codes.
+struct Fp4AppendArgs {
+  RotaryArgs r;
+  int hkv;
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+  int64_t ss_seq, ss_tok, ss_head;
+};
+hipError_t launch_fp4_append(const Fp4AppendArgs& a, bool interleaved, int cus, hipStream_t stream);
 
 struct SampleArgs {
   const void* logits;

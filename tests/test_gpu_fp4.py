@@ -1,0 +1,486 @@
+"""The 4-bit cache on the GPU against the float64 oracle: filled, read back and attended
+over.
+
+Filling: the turned key of the oracle is off by a few 2^-52, so a code differs only
+where the key lies within 1e-9 of its size of a border between two codes (or of two
+exponents); values are exact.  Reading back is exact.  Attention: the cache's values are
+exact numbers, so the tolerances are those of bf16 chunk attention over them."""
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.fp4 as fp4
+import oracle.rotary as rope
+import oracle.window as ref
+from test_gpu_window import near
+
+pytestmark = pytest.mark.gpu
+
+
+def f64(x):
+    return x.double().cpu().numpy()
+
+
+def decoded(cache):
+    c = [x.cpu().numpy() for x in cache]
+    return fp4.decode(c[0], c[2]), fp4.decode(c[1], c[3])
+
+
+def random_cache(shape, d, g, head_inner=False):
+    """Codes and scales of [n, tokens, hkv] heads, CPU tensors; every code, exponents
+    around 0."""
+    n, tokens, hkv = shape
+
+    def part(lo, hi, width):
+        if head_inner:
+            return torch.randint(lo, hi, (n, tokens, hkv, width), generator=g, dtype=torch.uint8)
+        return torch.randint(lo, hi, (n, hkv, tokens, width), generator=g, dtype=torch.uint8).transpose(1, 2)
+
+    return [part(0, 256, d // 2), part(0, 256, d // 2), part(124, 128, d // 32), part(124, 128, d // 32)]
+
+
+def to_gpu(x):
+    """With its strides."""
+    y = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device="cuda")
+    return y.copy_(x)
+
+
+def make(lens, hq, hkv, d, page, seed, first=0, pad=0, cap=None, head_inner=False):
+    """As in chunk attention's tests; entries past kv hold NaN (scale 255)."""
+    g = torch.Generator().manual_seed(seed)
+    b, cap = len(lens), cap or max(max(kv for _, kv in lens), 1)
+    n = [x for x, _ in lens]
+    T = first + sum(n) + pad
+    per = -(-cap // page) if page else 0
+    shape = (b * per + 1, page, hkv) if page else (b, cap, hkv)
+    cache = random_cache(shape, d, g, head_inner)
+    table = None
+    held = torch.zeros(shape[:2], dtype=torch.bool)
+    if page:
+        table = torch.randperm(b * per, generator=g).view(b, per).to(torch.int32)
+        for i, (_, x) in enumerate(lens):
+            for t in range(x):
+                held[int(table[i, t // page]), t % page] = True
+            table[i, -(-x // page):] = b * per
+    else:
+        held = torch.arange(cap) < torch.tensor([x for _, x in lens])[:, None]
+    cache[2][~held] = 255
+    cache[3][~held] = 255
+    return dict(q=torch.randn((T, hq, d), generator=g).bfloat16(), cache=cache, table=table, cap=cap, page=page, max_q=max(n),
+                starts=torch.tensor([first] + list(np.cumsum(n) + first), dtype=torch.int32),
+                kv=torch.tensor([x for _, x in lens], dtype=torch.int32))
+
+
+def call(s, **kw):
+    from paper_2606_02544_amd import binding
+    kw.setdefault("max_q_len", s["max_q"])
+    table = None if s["table"] is None else s["table"].cuda()
+    return binding.chunk_attention_fp4(s["q"].cuda(), binding.Fp4Cache(*map(to_gpu, s["cache"])), table, s["starts"].cuda(),
+                                       s["kv"].cuda(), max_kv_len=s["cap"], page_size=s["page"], **kw)
+
+
+def check(s, out, lse, mask_block, window=0, sinks=0, scale=0.0):
+    k, v = decoded(s["cache"])
+    want, wl, size, S = ref.chunk_attention(f64(s["q"]), k, v, s["table"], s["starts"].tolist(), s["kv"].tolist(),
+                                            mask_block=mask_block, window=window, sinks=sinks, page=s["page"], scale=scale)
+    rows = ~np.isnan(wl[0])
+    near(f64(out)[rows], f64(lse).T[rows], want[rows], wl.T[rows], size[rows], S.T[rows], s["q"].shape[2], s["cap"], True)
+
+
+# ---------------------------------------------------------------------------
+# Reading back
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("shape,d", [((1, 1, 1), 64), ((3, 5, 2), 128), ((7, 16, 8), 128), ((2, 1000, 3), 64), ((0, 4, 2), 64)])
+def test_values_of_every_code_and_scale(shape, d):
+    from paper_2606_02544_amd import binding
+    g = torch.Generator().manual_seed(1)
+    for head_inner in (False, True):
+        cache = random_cache(shape, d, g, head_inner)
+        for t in cache[2:]:
+            t.copy_(torch.randint(0, 256, t.shape, generator=g, dtype=torch.uint8))
+        k, v = binding.fp4_values(binding.Fp4Cache(*map(to_gpu, cache)))
+        for got, want in zip((k, v), decoded(cache)):
+            assert got.shape == (*shape, d) and got.dtype == torch.bfloat16 and got.is_contiguous()
+            # (past bf16's range, infinite)
+            with np.errstate(over="ignore"):
+                want = torch.from_numpy(want.astype(np.float32)).bfloat16()
+            got = got.cpu()
+            assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~got.isnan()], want[~want.isnan()])
+
+
+def test_values_past_32_bits():
+    """Codes and outputs whose offsets pass 2^32."""
+    from paper_2606_02544_amd import binding
+    n, hkv, d = 40, 2, 128
+    stride = 2 ** 32 // n // 16 * 16 + 1024
+    g = torch.Generator().manual_seed(2)
+    cache = random_cache((1, n, hkv), d, g)
+    want = binding.fp4_values(binding.Fp4Cache(*map(to_gpu, cache)))
+
+    def far(x, step):
+        y = torch.empty(step * (n - 1) + hkv * x.shape[3], dtype=torch.uint8, device="cuda")
+        y = torch.as_strided(y, x.shape, (0, step, x.shape[3], 1))
+        return y.copy_(x)
+
+    got = binding.fp4_values(binding.Fp4Cache(*[far(x, stride) for x in cache]))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    big = binding.fp4_cache(1, 2 ** 22 + 3, 8, 128)            # 2^32 output values and more
+    big.k[0, -1, 7] = 0x21
+    big.k_scales[0, -1, 7] = 127
+    out = torch.full((1, 2 ** 22 + 3, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    k, _ = binding.fp4_values(big, k_out=out, v_out=out)
+    assert not bool(out.any())
+    k, _ = binding.fp4_values(big, k_out=out)
+    assert k is out and not bool(out[0, :-1].any()) and not bool(out[0, -1, :7].any())
+    assert out[0, -1, 7].tolist() == [0.5, 1.0] * 64
+
+
+# ---------------------------------------------------------------------------
+# Filling
+# ---------------------------------------------------------------------------
+def same_codes(got_codes, got_scales, x, turned):
+    """Codes and scales of x [rows, heads, d] (float64): all of them, or, of turned keys,
+    but for those at a border."""
+    got = fp4.decode(got_codes, got_scales)
+    codes, scales = fp4.encode(x)
+    want = fp4.decode(codes, scales)
+    groups = np.abs(x).reshape(-1, 32)
+    e = np.repeat(scales.astype(np.int64).reshape(-1, 1) - 127, 32, 1)
+    with np.errstate(invalid="ignore"):
+        y = np.ldexp(groups, -e)
+        at = np.min(np.abs(y[..., None] - np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])), -1) <= 1e-9 * np.maximum(y, 1e-3)
+        top = np.ldexp(groups.max(1), -e[:, 0])
+        edge = (np.abs(top - 7.0) <= 7e-9) | (np.abs(top - 3.5) <= 4e-9)
+    edge &= turned
+    free = (turned & at | edge[:, None]).reshape(x.shape)
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    assert (same | free).all(), np.argwhere(~(same | free))[:5]
+    assert np.array_equal(got_scales.reshape(-1)[~edge], scales.reshape(-1)[~edge])
+
+
+def append(q, k, v, cache, table, starts, kv, freq, cap, page, **kw):
+    from paper_2606_02544_amd import binding
+    return binding.rotary_append_fp4(q, k, v, cache, table, starts, kv, freq, max_kv_len=cap, page_size=page, **kw)
+
+
+LENS = [([1], [1], 0, 0), ([3, 0, 5, 1], [3, 0, 100, 77], 0, 0), ([0, 0], [5, 0], 2, 3), ([1] * 70, list(range(1, 71)), 1, 2),
+        ([65, 7, 130], [65, 107, 131], 0, 9)]
+
+
+@pytest.mark.parametrize("d,rot,interleaved", [(128, 128, False), (128, 64, True), (64, 64, False), (64, 16, False),
+                                               (128, 36, False), (64, 6, True), (128, 2, False)])
+@pytest.mark.parametrize("page", [0, 1, 24])
+@pytest.mark.parametrize("lens,kv,first,pad", LENS)
+def test_append(d, rot, interleaved, page, lens, kv, first, pad):
+    from paper_2606_02544_amd import binding
+    hq, hkv = 3, 2
+    g = torch.Generator().manual_seed(len(lens) * 7 + rot)
+    T = first + sum(lens) + pad
+    x = (torch.randn((T, hq + 2 * hkv, d), generator=g) * torch.exp2(4 * torch.randn((T, 1, d), generator=g))).bfloat16()
+    q, k, v = x.cuda().split([hq, hkv, hkv], 1)
+    starts = torch.tensor([first] + list(np.cumsum(lens) + first), dtype=torch.int32)
+    cap = max(kv + [1])
+    per = -(-cap // page) if page else 0
+    n = (len(lens) * per + 1, page) if page else (len(lens), cap)
+    cache = binding.fp4_cache(*n, hkv, d)
+    for t in cache:
+        t.fill_(77)
+    table = torch.randperm(len(lens) * per, generator=g).view(len(lens), per).to(torch.int32) if page else None
+    freq, _ = binding.rope_frequencies(rot, 10000.0)
+    out = torch.full((T, hq, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    got = append(q, k, v, cache, table.cuda() if page else None, starts.cuda(), torch.tensor(kv, dtype=torch.int32).cuda(), freq,
+                 cap, page, interleaved=interleaved, attn_factor=1.25, q_out=out)
+    assert got is out
+    # Queries: the bits that the bf16 append gives.
+    bf = [torch.zeros((*n, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    want = torch.full_like(out, 9.0)
+    binding.rotary_append(q, k, v, *bf, table.cuda() if page else None, starts.cuda(), torch.tensor(kv, dtype=torch.int32).cuda(),
+                          freq, max_kv_len=cap, page_size=page, interleaved=interleaved, attn_factor=1.25, q_out=want)
+    assert torch.equal(out, want)
+    rows = rope.cache_rows(starts.tolist(), kv, T)
+    live = [t for t in range(T) if rows[t][0] >= 0 and rows[t][1] >= 0]
+    c = [t.cpu().numpy() for t in cache]
+    if live:
+        pos = np.array([rows[t][1] for t in live])
+        turned = rope.rotate(f64(k)[live], pos, freq.cpu().numpy(), interleaved=interleaved, factor=1.25)
+        at = [((int(table[b, i // page]), i % page) if page else (b, i)) for b, i in (rows[t] for t in live)]
+        pick = lambda a: np.stack([a[i] for i in at])  # noqa: E731
+        same_codes(pick(c[0]), pick(c[2]), turned, True)
+        same_codes(pick(c[1]), pick(c[3]), f64(v)[live], False)
+        for a in c:
+            for i in at:
+                a[i] = 77
+    assert all((a == 77).all() for a in c), "rows of no token were written"
+
+
+def test_append_of_many_tokens_and_positions():
+    """Four tokens a work-group; positions of the caller's; queries none."""
+    from paper_2606_02544_amd import binding
+    T, hkv, d = 8195, 1, 64
+    g = torch.Generator().manual_seed(5)
+    k, v = (torch.randn((T, hkv, d), generator=g).bfloat16().cuda() for _ in range(2))
+    pos = torch.randint(-5, 10 ** 6, (T,), generator=g, dtype=torch.int32)
+    freq, factor = binding.rope_frequencies(d, 1e6, scaling="yarn", factor=4.0, original_context=8192)
+    cache = binding.fp4_cache(1, T, hkv, d)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    assert append(None, k, v, cache, None, i32(0, T), i32(T), freq, T, 0, positions=pos.cuda(), attn_factor=factor) is None
+    c = [t.cpu().numpy()[0] for t in cache]
+    # (Angles up to 1e6 radians in fp64: 3 roundings of them, 4e-10, moves a key by that.)
+    turned = rope.rotate(f64(k), pos.numpy(), freq.cpu().numpy(), factor=factor)
+    same_codes(c[0], c[2], turned, True)
+    same_codes(c[1], c[3], f64(v), False)
+
+
+@pytest.mark.parametrize("seed", [0, 1])
+def test_append_of_borders_and_extremes(seed):
+    """Values on the borders between codes and between exponents, zeros, the type's
+    smallest and largest numbers, infinities and NaN; unturned keys (position 0) are
+    rounded as they are."""
+    from paper_2606_02544_amd import binding
+    d, T = 128, 400
+    g = np.random.RandomState(seed)
+    at = np.array([0.0, 0.25, 0.5, 0.75, 1.0, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 8.0, 6.5, 14.0])
+    x = at[g.randint(0, len(at), (T, 1, d))] * np.where(g.rand(T, 1, d) < 0.5, -1, 1)
+    x = x * 2.0 ** np.repeat(g.randint(-140, 125, (T, 1, d // 32)), 32, -1)
+    step = g.randint(-1, 2, x.shape)                           # a bf16 step beside the border
+    t = torch.from_numpy(x.astype(np.float32)).bfloat16()
+    bits = t.view(torch.int16).int()
+    bits = torch.where((bits & 0x7fff) > 1, bits + torch.from_numpy(step).int(), bits)
+    t = bits.to(torch.int16).view(torch.bfloat16)
+    t[0, 0, 5], t[1, 0, 40], t[2, 0, 127], t[3, 0, 0] = float("inf"), float("nan"), -float("inf"), 3.3e38
+    t[4] = 0.0
+    t[5] = -0.0
+    cache = binding.fp4_cache(1, T, 1, d)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    freq, _ = binding.rope_frequencies(2, 10000.0)
+    append(None, t.cuda(), t.cuda(), cache, None, i32(0, T), i32(T), freq, T, 0, positions=torch.zeros(T, dtype=torch.int32).cuda())
+    c = [a.cpu().numpy()[0] for a in cache]
+    codes, scales = fp4.encode(f64(t))
+    # (Dims 0 and 1 of a key turn by 0: an infinite one times sin 0 makes its pair NaN, whose 32 are NaN anyway.)
+    for i in range(2):
+        assert np.array_equal(c[2 + i], scales)
+        got, want = fp4.decode(c[i], c[2 + i]), fp4.decode(codes, scales)
+        assert np.array_equal(got, want, equal_nan=True)
+
+
+def test_append_refuses_rows_past_the_cache():
+    """Tokens whose cache row is outside the cache, or whose page is none, are not
+    written; their queries turn."""
+    from paper_2606_02544_amd import binding
+    g = torch.Generator().manual_seed(6)
+    q, k, v = torch.randn((10, 6, 64), generator=g).bfloat16().cuda().split([2, 2, 2], 1)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    freq, _ = binding.rope_frequencies(64, 10000.0)
+    cache = binding.fp4_cache(2, 8, 2, 64)
+    out = append(q, k, v, cache, None, i32(0, 5, 10), i32(10, 3), freq, 8, 0)
+    assert bool(out.abs().sum((1, 2)).all())
+    ks = cache.k_scales.cpu()
+    assert bool((ks[0, 5:8] > 0).all()) and not bool(ks[0, :5].any())       # rows 5..9 of a cache of 8
+    assert bool((ks[1, :3] > 0).all()) and not bool(ks[1, 3:].any())        # rows -2..2
+    paged = binding.fp4_cache(3, 4, 2, 64)
+    table = i32(1, 7, -1, 2).view(2, 2)
+    append(q, k, v, paged, table, i32(0, 5, 10), i32(5, 8), freq, 8, 4)
+    ks = paged.k_scales.cpu()
+    assert bool((ks[1] > 0).all()) and not bool(ks[0].any()) and bool((ks[2] > 0).all())
+
+
+def test_append_past_32_bits():
+    from paper_2606_02544_amd import binding
+    n, d = 40, 64
+    step = 2 ** 32 // n // 16 * 16 + 1024
+    g = torch.Generator().manual_seed(8)
+    k, v = (torch.randn((n, 1, d), generator=g).bfloat16().cuda() for _ in range(2))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    freq, _ = binding.rope_frequencies(d, 10000.0)
+    dense = binding.fp4_cache(1, n, 1, d)
+    append(None, k, v, dense, None, i32(0, n), i32(n), freq, n, 0)
+    far = binding.Fp4Cache(*[torch.as_strided(torch.zeros(step * (n - 1) + x.shape[3], dtype=torch.uint8, device="cuda"),
+                                              x.shape, (step * n, step, x.shape[3], 1)) for x in dense])
+    append(None, k, v, far, None, i32(0, n), i32(n), freq, n, 0)
+    assert all(torch.equal(a, b) for a, b in zip(far, dense))
+    q = torch.randn((2, 1, d), generator=g).bfloat16().cuda()
+    run = lambda c: binding.chunk_attention_fp4(q, c, None, i32(0, 2), i32(n), max_q_len=2, max_kv_len=n)  # noqa: E731
+    a, b = run(far), run(dense)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ---------------------------------------------------------------------------
+# Attention
+# ---------------------------------------------------------------------------
+SHAPES = [
+    ([(1, 1)], 1, 1), ([(1, 64)], 4, 2), ([(1, 65), (1, 1000), (1, 3)], 8, 2), ([(5, 5)], 4, 4),
+    ([(64, 64), (1, 130), (0, 50), (17, 140)], 8, 2), ([(100, 300)], 3, 1), ([(33, 33), (70, 200)], 16, 1),
+    ([(0, 0), (3, 3), (0, 7)], 2, 1), ([(300, 300)], 4, 1),
+]
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("lens,hq,hkv", SHAPES)
+def test_shapes(d, page, lens, hq, hkv):
+    s = make(lens, hq, hkv, d, page, 1)
+    for mask_block in (1, 8, 0):
+        check(s, *call(s, mask_block=mask_block), mask_block)
+    check(s, *call(s, mask_block=1, window=50, sinks=3), 1, 50, 3)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("page", [0, 1, 4, 5, 24, 64, 100, 256])
+@pytest.mark.parametrize("kv_chunk", [0, 64, 128])
+def test_pages_and_key_ranges(d, page, kv_chunk):
+    s = make([(7, 450), (40, 257), (1, 64)], 4, 2, d, page, 2, head_inner=page == 5)
+    check(s, *call(s, mask_block=4, kv_chunk=kv_chunk), 4)
+    check(s, *call(s, mask_block=4, kv_chunk=kv_chunk, window=130, sinks=70), 4, 130, 70)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("max_q", [1, 20, 40, 500])
+def test_every_group_shape(d, max_q):
+    s = make([(9, 70), (1, 333), (90, 200)], 8, 2, d, 16, 4)
+    for kv_chunk in (0, 128):
+        check(s, *call(s, mask_block=8, max_q_len=max_q, kv_chunk=kv_chunk), 8)
+
+
+@pytest.mark.parametrize("heads", [16, 64])
+@pytest.mark.parametrize("lens", [[(130, 150)], [(512, 512)], [(200, 230), (0, 40), (100, 100)]])
+def test_blocks_that_share_a_unit(heads, lens):
+    s = make(lens, heads, heads, 64, 0, 15)
+    check(s, *call(s, mask_block=8, kv_chunk=1024), 8)
+
+
+@pytest.mark.parametrize("batch,first", [(64, 3), (65, 3), (150, 0)])
+def test_many_sequences_rows_outside_and_negative_positions(batch, first):
+    s = make([(i % 4, max(0, i % 4 + (37 * i) % 90 - 1)) for i in range(batch)], 4, 2, 64, 16, 7, first=first, pad=first)
+    out = torch.full(s["q"].shape, 9.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((4, s["q"].shape[0]), 9.0, device="cuda")
+    for kv_chunk in (0, 64):
+        call(s, mask_block=1, kv_chunk=kv_chunk, out=out, lse=lse)
+        check(s, out, lse, 1)
+        T = s["q"].shape[0]
+        rows = list(range(first)) + list(range(T - first, T))
+        assert bool((out[rows] == 9.0).all()) and bool((lse[:, rows] == 9.0).all())
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("kv_chunk", [0, 64])
+@pytest.mark.parametrize("max_q", [1, 20, 40, 500])
+def test_keys_and_values_that_are_nan(d, kv_chunk, max_q):
+    """32 dims held as NaN: rows that see them have NaN there (a value) or everywhere (a
+    key), the others what they had."""
+    s = make([(60, 350), (1, 300)], 4, 2, d, 16, 31)
+    base, base_lse = call(s, mask_block=1, kv_chunk=kv_chunk, max_q_len=max_q)
+
+    def at(b, t):
+        return int(s["table"][b, t // 16]), t % 16
+
+    for b, t, group in ((0, 10, 0), (0, 320, 1), (1, 299, 1)):
+        s["cache"][3][(*at(b, t), 1, group)] = 255
+    out, lse = call(s, mask_block=1, kv_chunk=kv_chunk, max_q_len=max_q)
+    want = base.clone()
+    want[:60, 2:, :32] = float("nan")
+    want[30:60, 2:, 32:64] = float("nan")                      # 320 < 291 + i
+    want[60, 2:, 32:64] = float("nan")
+    same = (out == want) | (out.isnan() & want.isnan())
+    assert bool(same.all()), (~same).nonzero()[:8]
+    assert torch.equal(lse, base_lse)
+    s["cache"][2][(*at(0, 340), 0, 0)] = 255
+    again, again_lse = call(s, mask_block=1, kv_chunk=kv_chunk, max_q_len=max_q)
+    assert bool(again[50:60, :2].isnan().all()) and bool(again_lse[:2, 50:60].isnan().all())
+    assert torch.equal(again[:50, :2], out[:50, :2]) and torch.equal(again_lse[:, :50], lse[:, :50])
+
+
+def test_scales_of_every_size():
+    """Exponents from the smallest to such that scores stay finite, and a given scale."""
+    s = make([(20, 90)], 2, 1, 64, 0, 10)
+    g = torch.Generator().manual_seed(3)
+    s["cache"][2][0, :90] = torch.randint(2, 130, (90, 1, 2), generator=g, dtype=torch.uint8)
+    s["cache"][3][0, :90] = torch.randint(2, 150, (90, 1, 2), generator=g, dtype=torch.uint8)
+    check(s, *call(s, mask_block=1, scale=0.5), 1, scale=0.5)
+
+
+def test_one_cache_for_all_sequences_and_no_keys():
+    from paper_2606_02544_amd import binding
+    s = make([(3, 80), (2, 80)], 4, 2, 64, 0, 15)
+    s["cache"] = [x[:1].expand(2, -1, -1, -1) for x in s["cache"]]
+    shared = binding.Fp4Cache(*[to_gpu(x[:1]).expand(2, -1, -1, -1) for x in s["cache"]])
+    out, lse = binding.chunk_attention_fp4(s["q"].cuda(), shared, None, s["starts"].cuda(), s["kv"].cuda(), max_q_len=3, max_kv_len=80)
+    check(s, out, lse, 1)
+    zero = torch.zeros(2, dtype=torch.int32, device="cuda")
+    out, lse = binding.chunk_attention_fp4(s["q"].cuda(), None, None, s["starts"].cuda(), zero, max_q_len=3, max_kv_len=0)
+    assert not bool(out.any()) and bool(torch.isneginf(lse).all())
+
+
+def test_replays_of_two_graphs_threads_and_another_stream():
+    import threading
+    from paper_2606_02544_amd import binding
+    sets, graphs, outs = [], [], []
+    for seed in (1, 2, 3):
+        s = make([(3, 500), (1, 700)], 4, 2, 128, 0, 20 + seed)
+        s = {k: (x.cuda() if isinstance(x, torch.Tensor) else x) for k, x in s.items()}
+        sets.append(dict(s, cache=binding.Fp4Cache(*map(to_gpu, s["cache"]))))
+    run = lambda s, **kw: binding.chunk_attention_fp4(s["q"], s["cache"], None, s["starts"], s["kv"],  # noqa: E731
+                                                      max_q_len=3, max_kv_len=s["cap"], kv_chunk=64, **kw)
+    eager = [run(s) for s in sets]
+    for s in sets[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(run(s))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(4):
+        for o in outs:
+            o[0].fill_(5.0)
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        run(sets[0])
+        torch.cuda.synchronize()
+        for o, e in zip(outs, eager):
+            assert torch.equal(o[0], e[0]) and torch.equal(o[1], e[1])
+    streams[0].wait_stream(torch.cuda.current_stream())
+    got = run(sets[0], stream=streams[0])
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], eager[0][0]) and torch.equal(got[1], eager[0][1])
+    found = [[], [], []]
+    threads = [threading.Thread(target=lambda i=i: found[i].extend(run(sets[i]) for _ in range(30))) for i in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(3):
+        assert len(found[i]) == 30 and all(torch.equal(o, eager[i][0]) and torch.equal(x, eager[i][1]) for o, x in found[i])
+
+
+def test_append_captured_and_replayed():
+    """A decode step's append and attention in one graph, replayed while the cache grows,
+    eager calls between the replays."""
+    from paper_2606_02544_amd import binding
+    b, cap, hq, hkv, d = 3, 300, 4, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = torch.randn((b, hq + 2 * hkv, d), generator=g, device="cuda").bfloat16()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    starts, kv = i32(0, 1, 2, 3), i32(200, 1, 64)
+    freq, _ = binding.rope_frequencies(d, 10000.0)
+    mine, other = (binding.fp4_cache(b, cap, hkv, d) for _ in range(2))
+
+    def step(c):
+        q, k, v = rows.split([hq, hkv, hkv], 1)
+        q = append(q, k, v, c, None, starts, kv, freq, cap, 0)
+        return binding.chunk_attention_fp4(q, c, None, starts, kv, max_q_len=1, max_kv_len=cap, kv_chunk=64, window=90, sinks=4)
+
+    step(other)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(mine)
+    for _ in range(4):
+        copy = binding.Fp4Cache(*[x.clone(memory_format=torch.preserve_format) for x in mine])
+        want = step(copy)
+        graph.replay()
+        step(other)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((*got, *mine), (*want, *copy)))
+        kv += 1
+        rows.copy_(torch.randn(rows.shape, generator=g, device="cuda"))

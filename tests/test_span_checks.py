@@ -1,0 +1,315 @@
+"""What windows with sinks and the 4-bit cache refuse, the layout of their descriptors,
+and their oracles pinned by hand (CPU; no kernel is launched)."""
+
+import ctypes
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.chunk
+import oracle.fp4 as fp4
+import oracle.window as win
+from paper_2606_02544_amd import binding
+from paper_2606_02544_amd.binding import AttnDesc, Fp4Pointers, Fp4ValuesDesc
+from test_operator_checks import FAKE, NULL, chunk_desc, no_gpu, rotary_desc  # noqa: F401 (no_gpu: a fixture)
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BF, I32, U8 = torch.bfloat16, torch.int32, torch.uint8
+BAD = 2 ** 31 - 1
+
+
+# --- the C entries ------------------------------------------------------------
+@pytest.mark.skipif(shutil.which("gcc") is None, reason="gcc not available")
+def test_descriptor_layouts(tmp_path):
+    kinds = {"simsd_fp4_cache": Fp4Pointers, "simsd_fp4_values_desc": Fp4ValuesDesc}
+    lines = []
+    for name, cls in kinds.items():
+        lines += [f'printf("%zu\\n", offsetof({name}, {f[0]}));' for f in cls._fields_]
+        lines.append(f'printf("%zu\\n", sizeof({name}));')
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include "simsd.h"\nint main(void) {' + "\n".join(lines) + "return 0; }")
+    exe = str(tmp_path / "layout")
+    subprocess.run(["gcc", "-I" + os.path.join(ROOT, "include"), str(src), "-o", exe], check=True)
+    got = [int(x) for x in subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()]
+    want = []
+    for cls in kinds.values():
+        want += [getattr(cls, f[0]).offset for f in cls._fields_] + [ctypes.sizeof(cls)]
+    assert got == want
+
+
+def pointers(**kw):
+    d = dict(k=0x10000, v=0x10000, k_scales=0x10001, v_scales=0x10001, scale_stride_seq=512, scale_stride_token=4,
+             scale_stride_head=2)
+    d.update(kw)
+    return Fp4Pointers(**d)
+
+
+def chunk(form, desc, window=8, sinks=2, cache=Fp4Pointers, **over):
+    fn = getattr(binding.lib(), f"simsd_chunk_attention_{form}")
+    names = ("q",) + (("k_cache", "v_cache") if form == "window" else ("cache",)) + \
+        ("block_table", "q_starts", "kv_lens", "out", "lse", "workspace")
+    args = [over.get(n, FAKE) for n in names]
+    if form == "fp4":
+        args[1] = cache and ctypes.byref(pointers() if cache is Fp4Pointers else cache)
+    return fn(desc and ctypes.byref(desc), window, sinks, *args, 0, None)
+
+
+def verify_desc(**kw):
+    d = dict(batch=2, num_q_heads=4, num_kv_heads=2, head_dim=64, block_size=4, max_ref=4, max_prefix_len=32,
+             page_size=0, max_pages_per_seq=0, kv_chunk=0, cache_stride_seq=4096, cache_stride_token=128,
+             cache_stride_head=64, scale=0.0, dtype=1, rope_theta=0.0)
+    d.update(kw)
+    return AttnDesc(**d)
+
+
+def verify(form, desc, window=8, sinks=2, cache=Fp4Pointers, **over):
+    fn = getattr(binding.lib(), f"simsd_verify_attention_{form}")
+    names = ("q", "k_new", "v_new") + (("k_cache", "v_cache") if form == "window" else ("cache",)) + \
+        ("block_table", "prefix_lens", "step_map", "num_ref", "out", "lse", "workspace")
+    args = [over.get(n, FAKE) for n in names]
+    if form == "fp4":
+        args[3] = cache and ctypes.byref(pointers() if cache is Fp4Pointers else cache)
+    return fn(desc and ctypes.byref(desc), window, sinks, *args, 0, None)
+
+
+@pytest.mark.parametrize("form", ["window", "fp4"])
+@pytest.mark.parametrize("window,sinks", [(-1, 0), (0, 1), (8, -1), (-2 ** 31, 0)])
+def test_windows_that_are_none(no_gpu, form, window, sinks):
+    assert chunk(form, chunk_desc(), window, sinks) == 2
+    assert verify(form, verify_desc(), window, sinks) == 2
+    sized = binding.lib().simsd_chunk_attention_window_workspace_size
+    assert sized(ctypes.byref(chunk_desc(max_kv_len=100000)), window, sinks) == 0
+
+
+@pytest.mark.parametrize("form", ["window", "fp4"])
+def test_descriptors(no_gpu, form):
+    assert chunk(form, None) == 1 and verify(form, None) == 1
+    assert chunk(form, chunk_desc(mask_block=0)) == 2 and b"mask_block" in binding.lib().simsd_last_error()
+    for field, value, status in (("num_tokens", -1, 2), ("batch", 0, 2), ("head_dim", 96, 3), ("max_kv_len", -1, 2),
+                                 ("page_size", -1, 2), ("kv_chunk", 65, 2), ("kv_chunk", -64, 2), ("cache_stride_token", 4, 4),
+                                 ("scale", float("nan"), 2), ("dtype", 9, 3), ("num_q_heads", 5, 2)):
+        assert chunk(form, chunk_desc(**{field: value})) == status, field
+    for field, value, status in (("batch", 0, 2), ("head_dim", 96, 3), ("max_prefix_len", -1, 2), ("kv_chunk", -1, 3),
+                                 ("kv_chunk", 65, 2), ("dtype", 0, 3), ("rope_theta", 10000.0, 3), ("max_ref", 5, 2),
+                                 ("cache_stride_seq", -8, 2), ("batch", 2 ** 21, 2), ("max_prefix_len", BAD, 2)):
+        assert verify(form, verify_desc(**{field: value})) == status, field
+    if form == "fp4":
+        assert chunk(form, chunk_desc(dtype=0)) == 3
+        assert chunk(form, chunk_desc(cache_stride_token=8)) == 4 and verify(form, verify_desc(cache_stride_head=8)) == 4
+
+
+@pytest.mark.parametrize("form", ["window", "fp4"])
+def test_pointers(no_gpu, form):
+    c, v = chunk_desc(), verify_desc()
+    for n in ("q", "q_starts", "kv_lens", "out"):
+        assert chunk(form, c, **{n: NULL}) == 1, n
+    for n in ("q", "k_new", "v_new", "prefix_lens", "step_map", "num_ref", "out"):
+        assert verify(form, v, **{n: NULL}) == 1, n
+    paged = dict(page_size=16, max_pages_per_seq=2)
+    assert chunk(form, chunk_desc(**paged), block_table=NULL) == 1
+    assert verify(form, verify_desc(**paged), block_table=NULL) == 1
+    for n, at in (("q", 8), ("out", 8), ("q_starts", 2), ("kv_lens", 1), ("lse", 2)):
+        assert chunk(form, c, **{n: ctypes.c_void_p(0x10000 + at)}) == 4, n
+    for n, at in (("q", 8), ("k_new", 8), ("out", 8), ("prefix_lens", 2), ("step_map", 1), ("num_ref", 2), ("lse", 2)):
+        assert verify(form, v, **{n: ctypes.c_void_p(0x10000 + at)}) == 4, n
+    if form == "window":
+        for n in ("k_cache", "v_cache"):
+            assert chunk(form, c, **{n: NULL}) == 1 and verify(form, v, **{n: NULL}) == 1
+            assert chunk(form, c, **{n: ctypes.c_void_p(0x10008)}) == 4
+    else:
+        assert chunk(form, c, cache=NULL) == 1 and verify(form, v, cache=NULL) == 1
+        for n in ("k", "v", "k_scales", "v_scales"):
+            assert chunk("fp4", c, 8, 2, pointers(**{n: 0})) == 1, n
+            assert verify("fp4", v, 8, 2, pointers(**{n: 0})) == 1, n
+        assert chunk("fp4", c, 8, 2, pointers(v=0x10008)) == 4
+        assert chunk("fp4", c, 8, 2, pointers(scale_stride_token=-1)) == 2
+        assert verify("fp4", v, 8, 2, pointers(scale_stride_head=2 ** 48 + 1)) == 2
+    # a workspace that is missing or short
+    assert chunk(form, chunk_desc(kv_chunk=64, max_kv_len=640), 640, 0, workspace=NULL) == 5
+    assert chunk(form, chunk_desc(kv_chunk=64, max_kv_len=640), 640, 0) == 5
+    assert verify(form, verify_desc(kv_chunk=64, max_prefix_len=640), 640, 0) == 5
+    # nothing to do
+    assert chunk(form, chunk_desc(num_tokens=0), q=NULL, q_starts=NULL) == 0
+
+
+def fp4_append(desc, cache=Fp4Pointers, **over):
+    fn = binding.lib().simsd_rotary_append_fp4
+    names = ("q", "k", "v", "positions", "freq", "q_out", "cache", "block_table", "q_starts", "kv_lens")
+    args = [over.get(n, FAKE) for n in names]
+    args[6] = cache and ctypes.byref(pointers() if cache is Fp4Pointers else cache)
+    return fn(desc and ctypes.byref(desc), *args, None)
+
+
+def test_append(no_gpu):
+    d = rotary_desc()
+    assert fp4_append(None) == 1 and fp4_append(d, cache=NULL) == 1
+    for n in ("q", "k", "v", "freq", "q_out", "q_starts", "kv_lens"):
+        assert fp4_append(d, **{n: NULL}) == 1, n
+    for n in ("k", "v", "k_scales", "v_scales"):
+        assert fp4_append(d, pointers(**{n: 0})) == 1, n
+    wide = dict(q_out_stride_head=256, q_out_stride_token=1024)
+    assert fp4_append(rotary_desc(head_dim=72, **wide)) == 3 and fp4_append(rotary_desc(head_dim=256, **wide)) == 3
+    for field, value, status in (("dtype", 0, 3), ("num_kv_heads", 0, 2), ("cache_stride_token", 24, 4), ("rotary_dim", 7, 2), ("attn_factor", 0.0, 2)):
+        assert fp4_append(rotary_desc(**{field: value})) == status, field
+    # rows of codes (32 bytes a head) or of scales (2) that overlap
+    assert fp4_append(rotary_desc(cache_stride_head=16)) == 2
+    assert fp4_append(rotary_desc(cache_stride_token=32)) == 2
+    assert fp4_append(d, pointers(scale_stride_head=1)) == 2 and fp4_append(d, pointers(scale_stride_token=2)) == 2
+    assert fp4_append(d, pointers(scale_stride_head=64, scale_stride_token=2), k=NULL) == 1     # (apart: tokens inside heads)
+    assert fp4_append(rotary_desc(num_tokens=0), k=NULL, v=NULL) == 0
+
+
+def test_values(no_gpu):
+    def run(codes=FAKE, scales=FAKE, out=FAKE, **kw):
+        d = dict(n0=2, n1=3, n2=4, head_dim=64, code_stride=(384, 128, 32), scale_stride=(24, 8, 2))
+        d.update(kw)
+        d["code_stride"], d["scale_stride"] = ((ctypes.c_int64 * 3)(*d[n]) for n in ("code_stride", "scale_stride"))
+        return binding.lib().simsd_fp4_values(ctypes.byref(Fp4ValuesDesc(**d)), codes, scales, out, None)
+
+    assert binding.lib().simsd_fp4_values(None, FAKE, FAKE, FAKE, None) == 1
+    for kw, status in ((dict(n0=-1), 2), (dict(n1=-1), 2), (dict(n0=2 ** 31), 2), (dict(n0=2 ** 20, n1=2 ** 16, n2=2), 2),
+                       (dict(head_dim=48), 3), (dict(head_dim=544), 3), (dict(code_stride=(384, 130, 32)), 4),
+                       (dict(scale_stride=(24, -8, 2)), 2), (dict(code_stride=(2 ** 49, 4, 4)), 2), (dict(codes=NULL), 1),
+                       (dict(scales=NULL), 1), (dict(out=NULL), 1), (dict(codes=ctypes.c_void_p(0x10002)), 4),
+                       (dict(out=ctypes.c_void_p(0x10008)), 4)):
+        assert run(**kw) == status, kw
+    assert run(n0=0, codes=NULL) == 0 and run(n2=0) == 0
+
+
+# --- the binding ----------------------------------------------------------------
+def cpu_cache(n=2, tokens=32, hkv=2, d=64):
+    return binding.fp4_cache(n, tokens, hkv, d, device="cpu")
+
+
+def test_fp4_cache():
+    c = cpu_cache(3, 16, 4, 128)
+    assert c.k.shape == c.v.shape == (3, 16, 4, 64) and c.k_scales.shape == (3, 16, 4, 4)
+    assert c.k.stride() == (4096, 64, 1024, 1) and c.k_scales.stride() == (256, 4, 64, 1)
+    with pytest.raises(ValueError, match="head_dim"):
+        binding.fp4_cache(1, 1, 1, 96, device="cpu")
+
+
+def broken(**kw):
+    return cpu_cache()._replace(**kw)
+
+
+@pytest.mark.parametrize("cache,match", [
+    (None, "Fp4Cache"), ((1, 2), "Fp4Cache"), (broken(k=torch.zeros(2, 32, 2, 32)), "uint8"),
+    (broken(v=None), "4-D"), (broken(k=torch.zeros((2, 32, 2, 32), dtype=U8)), "strides of the keys"),
+    (broken(v_scales=torch.zeros((2, 32, 2, 2), dtype=U8)), "scales differ"),
+    (cpu_cache(d=128), "heads of 128"), (cpu_cache(n=3), "dimension 0"), (cpu_cache(tokens=31), "holds 31"),
+    (binding.Fp4Cache(*[t[..., :1] for t in cpu_cache()]), "32|heads of"),
+])
+def test_caches(cache, match):
+    q, starts, kv = torch.zeros((3, 4, 64), dtype=BF), torch.zeros(3, dtype=I32), torch.zeros(2, dtype=I32)
+    with pytest.raises(ValueError, match=match):
+        binding.chunk_attention_fp4(q, cache, None, starts, kv, max_q_len=3, max_kv_len=32)
+    k = torch.zeros((3, 2, 64), dtype=BF)
+    with pytest.raises(ValueError, match=match):
+        binding.rotary_append_fp4(None, k, k, cache, None, starts, kv, torch.ones(32, dtype=torch.float64), max_kv_len=32)
+    new = torch.zeros((2, 8, 2, 64), dtype=BF)
+    with pytest.raises(ValueError, match=match):
+        binding.verify_attention_fp4(torch.zeros((2, 8, 4, 64), dtype=BF), new, new, cache, None, kv,
+                                     torch.zeros((2, 4), dtype=I32), kv, block_size=4, max_ref=4, max_prefix_len=32)
+
+
+def test_types_heads_and_devices():
+    c, starts, kv = cpu_cache(), torch.zeros(3, dtype=I32), torch.zeros(2, dtype=I32)
+    f = torch.ones(32, dtype=torch.float64)
+    q, k = torch.zeros((3, 4, 64), dtype=BF), torch.zeros((3, 2, 64), dtype=BF)
+    with pytest.raises(ValueError, match="bfloat16"):
+        binding.chunk_attention_fp4(q.float(), c, None, starts, kv, max_q_len=3, max_kv_len=32)
+    with pytest.raises(ValueError, match="bfloat16"):
+        binding.rotary_append_fp4(None, k.float(), k.float(), c, None, starts, kv, f, max_kv_len=32)
+    with pytest.raises(ValueError, match="KV heads"):
+        binding.rotary_append_fp4(None, k[:, :1], k[:, :1], c, None, starts, kv, f, max_kv_len=32)
+    with pytest.raises(ValueError, match="expanded"):
+        shared = binding.Fp4Cache(*[t[:1].expand(2, -1, -1, -1) for t in c])
+        binding.rotary_append_fp4(None, k, k, shared, None, starts, kv, f, max_kv_len=32)
+    with pytest.raises(ValueError, match="page_size"):
+        binding.chunk_attention_fp4(q, c, torch.zeros((2, 2), dtype=I32), starts, kv, max_q_len=3, max_kv_len=32, page_size=16)
+    with pytest.raises(ValueError, match="too few pages"):
+        binding.chunk_attention_fp4(q, c, torch.zeros((2, 1), dtype=I32), starts, kv, max_q_len=3, max_kv_len=64, page_size=32)
+    with pytest.raises(ValueError, match="block_table"):
+        binding.chunk_attention_fp4(q, c, None, starts, kv, max_q_len=3, max_kv_len=32, page_size=32)
+    with pytest.raises(ValueError, match="contiguous"):
+        binding.chunk_attention_fp4(torch.zeros((3, 8, 64), dtype=BF)[:, ::2], c, None, starts, kv, max_q_len=3, max_kv_len=32)
+    # all in order but for the device
+    with pytest.raises(ValueError, match="GPU"):
+        binding.chunk_attention_fp4(q, c, None, starts, kv, max_q_len=3, max_kv_len=32)
+    with pytest.raises(ValueError, match="GPU"):
+        binding.rotary_append_fp4(q, k, k, c, None, starts, kv, f, max_kv_len=32)
+    with pytest.raises(ValueError, match="GPU"):
+        binding.fp4_values(c)
+    cache = torch.zeros((2, 32, 2, 64), dtype=BF)
+    with pytest.raises(ValueError, match="GPU"):
+        binding.chunk_attention(q, cache, cache, None, starts, kv, max_q_len=3, max_kv_len=32, window=4, sinks=1)
+    for bad in (2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.chunk_attention(q, cache, cache, None, starts, kv, max_q_len=3, max_kv_len=32, window=bad)
+    with pytest.raises(TypeError):
+        binding.chunk_attention(q, cache, cache, None, starts, kv, max_q_len=3, max_kv_len=32, window=4.5)
+    new = torch.zeros((2, 8, 2, 64), dtype=BF)
+    rest = (None, kv, torch.zeros((2, 4), dtype=I32), kv)
+    sizes = dict(block_size=4, max_ref=4, max_prefix_len=32)
+    with pytest.raises(ValueError, match="GPU"):
+        binding.verify_attention(torch.zeros((2, 8, 4, 64), dtype=BF), new, new, cache, cache, *rest, **sizes, window=4)
+    with pytest.raises(ValueError, match="GPU"):
+        binding.verify_attention_fp4(torch.zeros((2, 8, 4, 64), dtype=BF), new, new, c, *rest, **sizes)
+    with pytest.raises(ValueError, match="descriptor"):
+        binding.verify_attention(torch.zeros((2, 8, 4, 64), dtype=BF), new, new, cache, cache, *rest, **sizes, window=4, desc=verify_desc())
+
+
+# --- the oracles ------------------------------------------------------------------
+def test_visible_keys_by_hand():
+    # 10 cached, 4 of them new: positions 6..9
+    assert win.keys(10, 4, 0, 1, 3, 0) == [4, 5, 6]
+    assert win.keys(10, 4, 3, 1, 3, 2) == [0, 1, 7, 8, 9]
+    assert win.keys(10, 4, 1, 4, 3, 1) == [0, 2, 3, 4, 5, 6, 7]         # block 4..7, two keys before it
+    assert win.keys(10, 4, 2, 4, 1, 0) == [8, 9]
+    assert win.keys(10, 4, 2, 1, 0, 0) == list(range(9))
+    assert win.keys(3, 5, 1, 1, 2, 1) == []                             # position -1
+    assert win.keys(10, 1, 0, 1, 100, 5) == list(range(10))
+
+
+def test_window_oracle_is_the_chunk_oracle_without_one():
+    g = np.random.RandomState(1)
+    q, k, v = g.randn(7, 4, 8), g.randn(2, 9, 2, 8), g.randn(2, 9, 2, 8)
+    for m in (1, 4, 0):
+        a = oracle.chunk.chunk_attention(q, k, v, None, [0, 3, 7], [9, 6], mask_block=m)
+        for w in (0, 50) if m else (0,):
+            b = win.chunk_attention(q, k, v, None, [0, 3, 7], [9, 6], mask_block=m, window=w)
+            for x, y in zip(a, b):
+                np.testing.assert_allclose(x, y, rtol=1e-13, atol=1e-13)
+
+
+def test_fp4_by_hand():
+    x = np.zeros((1, 32))
+    x[0, :12] = [6.9, 0.25, 0.26, 0.75, -1.25, 1.3, 1.75, 2.5, 2.6, 3.5, -5.0, 5.1]
+    codes, scales = fp4.encode(x)
+    assert scales.tolist() == [[127]]
+    assert fp4.decode(codes, scales)[0, :12].tolist() == [6, 0, 0.5, 1, -1, 1.5, 2, 2, 3, 4, -4, 6]
+    assert codes[0, 0] == 7 and codes[0, 1] == 1 + 16 * 2 and codes[0, 2] == 8 + 2 + 16 * 3
+    x[0, 0] = 7.0                                              # the next power of two
+    codes, scales = fp4.encode(x)
+    assert scales.tolist() == [[128]]
+    assert fp4.decode(codes, scales)[0, :4].tolist() == [8, 0, 0, 1]    # 3.5 -> 4, 0.125 -> 0, 0.13 -> 0, 0.375 -> 0.5
+    x[0, 5] = np.nan
+    codes, scales = fp4.encode(x)
+    assert scales.tolist() == [[255]] and np.isnan(fp4.decode(codes, scales)).all()
+    assert fp4.exponent(0.0) == -125 and fp4.exponent(2.0 ** 127) == 125 and fp4.exponent(2.0 ** -140) == -125
+    assert fp4.exponent(6.99) == 0 and fp4.exponent(7.0) == 1 and fp4.exponent(3.49) == -1
+
+
+def test_fp4_encodes_its_own_values():
+    g = np.random.RandomState(2)
+    codes = g.randint(0, 256, (50, 16), dtype=np.uint8)
+    codes[:, 0] = codes[:, 0] & 0xf0 | 7                       # one of each 32 is the largest, so the exponent stays
+    scales = g.randint(2, 253, (50, 1)).astype(np.uint8)
+    x = fp4.decode(codes, scales)
+    again = fp4.encode(x)
+    assert np.array_equal(again[1], scales) and np.array_equal(fp4.decode(*again), x)
