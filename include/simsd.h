@@ -591,9 +591,10 @@ simsd_status simsd_verify_attention_window(const simsd_attn_desc* desc, int32_t 
 typedef struct {
   void* k;                    /* codes, 16-byte aligned                           */
   void* v;
-  void* k_scales;             /* scales, no alignment                             */
+  void* k_scales;             /* scales, aligned to head_dim / 32 bytes           */
   void* v_scales;
-  int64_t scale_stride_seq;   /* bytes between sequences (contiguous) / pages     */
+  int64_t scale_stride_seq;   /* bytes between sequences (contiguous) / pages; all
+                                 three are multiples of head_dim / 32             */
   int64_t scale_stride_token;
   int64_t scale_stride_head;
 } simsd_fp4_cache;
@@ -641,22 +642,24 @@ simsd_status simsd_verify_attention_fp4(const simsd_attn_desc* desc, int32_t win
                                         const int32_t* num_ref, void* out, float* lse,
                                         void* workspace, size_t workspace_bytes, void* stream);
 
-/* Codes [n0, n1, n2, head_dim / 2] and scales [n0, n1, n2, head_dim / 32] of a cache's
- * keys or values, with strides in bytes. */
+/* A 4-bit cache as a whole: [num, tokens, num_kv_heads] heads. */
 typedef struct {
-  int64_t n0;                 /* sequences or pages, 0..2^31 - 1                  */
-  int32_t n1, n2;             /* tokens and heads, >= 0; n0 * n1 * n2 <= 2^36     */
+  int32_t num;                /* sequences or pages, >= 0                         */
+  int32_t tokens;             /* of each, >= 0                                    */
+  int32_t num_kv_heads;       /* >= 0; num * tokens * num_kv_heads <= 2^36        */
   int32_t head_dim;           /* a multiple of 32, 32..512                        */
-  int64_t code_stride[3];     /* multiples of 4                                   */
-  int64_t scale_stride[3];
+  int64_t cache_stride_seq;   /* of the codes, in bytes, multiples of 16          */
+  int64_t cache_stride_token;
+  int64_t cache_stride_head;
 } simsd_fp4_values_desc;
 
 /*
- * out [n0, n1, n2, head_dim] bf16, 16-byte aligned: the codes' values.  Exact; past
- * bf16's range infinite (no append writes such).  codes 4-byte aligned.  One kernel.
+ * The values of a cache's keys and of its values: k_out and v_out [num, tokens,
+ * num_kv_heads, head_dim] bf16, 16-byte aligned, each or NULL.  Exact; past bf16's
+ * range infinite (no append writes such).  One kernel.
  */
-simsd_status simsd_fp4_values(const simsd_fp4_values_desc* desc, const void* codes,
-                              const void* scales, void* out, void* stream);
+simsd_status simsd_fp4_values(const simsd_fp4_values_desc* desc, const simsd_fp4_cache* cache,
+                              void* k_out, void* v_out, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Sampling                                                                   */

@@ -83,9 +83,9 @@ class Fp4Pointers(ctypes.Structure):
 
 
 class Fp4ValuesDesc(ctypes.Structure):
-    _fields_ = [("n0", ctypes.c_int64), ("n1", ctypes.c_int32), ("n2", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32), ("code_stride", ctypes.c_int64 * 3),
-                ("scale_stride", ctypes.c_int64 * 3)]
+    _fields_ = [(n, ctypes.c_int32) for n in ("num", "tokens", "num_kv_heads", "head_dim")] + \
+               [(n, ctypes.c_int64) for n in
+                ("cache_stride_seq", "cache_stride_token", "cache_stride_head")]
 
 
 class SimsdError(RuntimeError):
@@ -164,7 +164,8 @@ def lib() -> ctypes.CDLL:
         L.simsd_rotary_append_fp4.argtypes = [ctypes.POINTER(RotaryDesc)] + [_P] * 6 + \
             [ctypes.POINTER(Fp4Pointers)] + [_P] * 4
         L.simsd_rotary_append_fp4.restype = ctypes.c_int
-        L.simsd_fp4_values.argtypes = [ctypes.POINTER(Fp4ValuesDesc)] + [_P] * 4
+        L.simsd_fp4_values.argtypes = [ctypes.POINTER(Fp4ValuesDesc), ctypes.POINTER(Fp4Pointers),
+                                       _P, _P, _P]
         L.simsd_fp4_values.restype = ctypes.c_int
         L.simsd_validate_step_map.argtypes = [_I32P, _I32P, ctypes.c_int32, ctypes.c_int32,
                                               ctypes.c_int32]
@@ -1039,8 +1040,30 @@ def fp4_cache(num: int, tokens: int, num_kv_heads: int, head_dim: int, *, device
     return Fp4Cache(part(head_dim // 2), part(head_dim // 2), part(head_dim // 32), part(head_dim // 32))
 
 
+def _fp4_short(cache, device):
+    """Shape and strides of a cache's codes and strides of its scales if everything that
+    _fp4_parts checks holds, else None."""
+    try:
+        k, v, ks, vs = cache
+        shape, st, ss = k.shape, k.stride(), ks.stride()
+        n, tokens, hkv, half = shape
+        small = (n, tokens, hkv, half // 16)
+        if (k.dtype is v.dtype is ks.dtype is vs.dtype is torch.uint8 and v.shape == shape
+                and v.stride() == st and vs.stride() == ss and ks.shape == small and vs.shape == small
+                and st[3] == ss[3] == 1 and half % 16 == 0 and k.device == device and v.device == device
+                and ks.device == device and vs.device == device):
+            return shape, st, ss
+    except (AttributeError, TypeError, ValueError, IndexError):
+        pass
+    return None
+
+
 def _fp4_parts(cache, device, width: int = 0):
-    """Shape of a cache's codes, which with its scales passes the checks here."""
+    """Shape and strides of a cache's codes and strides of its scales, which pass the
+    checks here."""
+    found = _fp4_short(cache, device)
+    if found is not None and isinstance(cache, tuple) and width in (0, 2 * found[0][3]):
+        return found
     if not isinstance(cache, tuple) or len(cache) != 4:
         _raise("cache must be an Fp4Cache (codes and scales of keys and values)")
     for name, t in zip(Fp4Cache._fields, cache):
@@ -1062,31 +1085,38 @@ def _fp4_parts(cache, device, width: int = 0):
         _raise(f"the codes hold heads of {2 * half} dims" + (f", expected {width}" if width else ": need a multiple of 32"))
     if ks.shape != (n, tokens, hkv, half // 16):
         _raise(f"the scales have shape {tuple(ks.shape)}, expected {(n, tokens, hkv, half // 16)}")
-    return k.shape
+    return k.shape, k.stride(), ks.stride()
 
 
-def _fp4_pointers(cache: Fp4Cache):
-    st = cache.k_scales.stride()
-    return Fp4Pointers(cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scales.data_ptr(),
-                       cache.v_scales.data_ptr(), st[0], st[1], st[2])
+def _fp4_pointers(cache: Fp4Cache, ss):
+    k, v, ks, vs = cache
+    return Fp4Pointers(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), ss[0], ss[1], ss[2])
 
 
 def _fp4_call(cache, device, d, page_size, max_len, batch, block_table):
-    """KV heads, pointers, strides and pages per sequence of a call's 4-bit cache."""
+    """KV heads, pointers, strides and pages per sequence of a call's 4-bit cache, and
+    whether its rows lie apart."""
     if max_len <= 0:
-        return None, Fp4Pointers(), (0, 0, 0), 0
-    n, tokens, hkv, _ = _fp4_parts(cache, device, d)
+        return None, Fp4Pointers(), (0, 0, 0), 0, True
+    (n, tokens, hkv, _), st, ss = _fp4_parts(cache, device, d)
     pages = 0
     if page_size > 0:
-        _need(tokens == page_size, f"paged cache: dimension 1 is {tokens}, page_size is {page_size}")
-        _need(block_table is not None, "paged cache needs a block_table")
+        if tokens != page_size:
+            _raise(f"paged cache: dimension 1 is {tokens}, page_size is {page_size}")
+        if block_table is None:
+            _raise("paged cache needs a block_table")
         _int32("block_table", block_table, (batch, None), device)
         pages = block_table.shape[1]
-        _need(pages * page_size >= max_len, "block_table has too few pages per sequence")
+        if pages * page_size < max_len:
+            _raise("block_table has too few pages per sequence")
     else:
-        _need(n == batch, f"contiguous cache: dimension 0 is {n}, batch is {batch}")
-        _need(tokens >= max_len, f"contiguous cache holds {tokens} tokens, need {max_len}")
-    return hkv, _fp4_pointers(cache), cache.k.stride()[:3], pages
+        if n != batch:
+            _raise(f"contiguous cache: dimension 0 is {n}, batch is {batch}")
+        if tokens < max_len:
+            _raise(f"contiguous cache holds {tokens} tokens, need {max_len}")
+    apart = not ((n > 1 and not (st[0] and ss[0])) or (tokens > 1 and not (st[1] and ss[1]))
+                 or (hkv > 1 and not (st[2] and ss[2])))
+    return hkv, _fp4_pointers(cache, ss), st[:3], pages, apart
 
 
 @functools.lru_cache(maxsize=1024)
@@ -1162,7 +1192,7 @@ def chunk_attention_fp4(q, cache: Optional[Fp4Cache], block_table, q_starts, kv_
     b = _ragged(q_starts, kv_lens, q.device)
     max_q_len, max_kv_len, page_size, mask_block, kv_chunk = map(
         operator.index, (max_q_len, max_kv_len, page_size, mask_block, kv_chunk))
-    hkv, pointers, cs, pages = _fp4_call(cache, q.device, q.shape[2], page_size, max_kv_len, b, block_table)
+    hkv, pointers, cs, pages, _ = _fp4_call(cache, q.device, q.shape[2], page_size, max_kv_len, b, block_table)
     return _chunk_span("fp4", q, (ctypes.byref(pointers),), cs, pages, block_table, q_starts, kv_lens, b,
                        q.shape[1] if hkv is None else hkv, max_q_len, max_kv_len, page_size, mask_block,
                        kv_chunk, scale, window, sinks, out, lse, want_lse, workspace, stream)
@@ -1202,11 +1232,14 @@ def verify_attention_fp4(q, k_new, v_new, cache: Optional[Fp4Cache], block_table
                          want_lse: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
     """simsd_verify_attention_fp4 on torch tensors: verify_attention over a 4-bit
     prefix.  Returns (out, lse)."""
-    hkv = check_attention_tensors(q, k_new, v_new, None, None, block_table, prefix_lens, step_map, num_ref,
-                                  out, lse, block_size=block_size, max_ref=max_ref, max_prefix_len=0,
-                                  page_size=page_size)
+    hkv = _attention_hkv(q, k_new, v_new, None, None, block_table, prefix_lens, step_map, num_ref, out, lse,
+                         block_size, max_ref, 0, page_size)
+    if hkv is None:
+        hkv = check_attention_tensors(q, k_new, v_new, None, None, block_table, prefix_lens, step_map, num_ref,
+                                      out, lse, block_size=block_size, max_ref=max_ref, max_prefix_len=0,
+                                      page_size=page_size)
     b, _, _, d = q.shape
-    held, pointers, cs, pages = _fp4_call(cache, q.device, d, operator.index(page_size),
+    held, pointers, cs, pages, _ = _fp4_call(cache, q.device, d, operator.index(page_size),
                                           operator.index(max_prefix_len), b, block_table)
     if held is not None and held != hkv:
         _raise(f"the cache has {held} KV heads, k_new has {hkv}")
@@ -1239,11 +1272,11 @@ def rotary_append_fp4(q, k, v, cache: Fp4Cache, block_table, q_starts, kv_lens, 
     ks, vs = _heads("k", k, (T, hkv, d), dt, dev), _heads("v", v, (T, hkv, d), dt, dev)
     b = _ragged(q_starts, kv_lens, dev)
     page_size, max_kv_len = operator.index(page_size), operator.index(max_kv_len)
-    held, pointers, cs, pages = _fp4_call(cache, dev, d, page_size, max_kv_len, b, block_table)
+    held, pointers, cs, pages, apart = _fp4_call(cache, dev, d, page_size, max_kv_len, b, block_table)
     if held is not None:
         if held != hkv:
             _raise(f"the cache has {held} KV heads, k has {hkv}")
-        if any(n > 1 and st == 0 for t in cache for n, st in zip(t.shape, t.stride())):
+        if not apart:
             _raise("the cache must not be an expanded tensor: its rows are written")
     if positions is not None:
         _vector("positions", positions, T, torch.int32, dev)
@@ -1261,28 +1294,32 @@ def rotary_append_fp4(q, k, v, cache: Fp4Cache, block_table, q_starts, kv_lens, 
     return q_out
 
 
+@functools.lru_cache(maxsize=1024)
+def _fp4_values_desc(*fields) -> Fp4ValuesDesc:
+    return _filled(Fp4ValuesDesc, fields)
+
+
 def fp4_values(cache: Fp4Cache, *, k_out: Optional[torch.Tensor] = None,
                v_out: Optional[torch.Tensor] = None, stream=None):
-    """simsd_fp4_values of a cache's keys and of its values: (k, v), bf16
+    """simsd_fp4_values: the values of a cache's keys and of its values, (k, v), bf16
     [seq or page, token, Hkv, d], contiguous."""
     if not isinstance(cache, tuple) or len(cache) != 4 or not isinstance(cache[0], torch.Tensor):
         _raise("cache must be an Fp4Cache (codes and scales of keys and values)")
     dev = cache[0].device
-    n, tokens, hkv, half = _fp4_parts(cache, dev)
+    (n, tokens, hkv, half), st, ss = _fp4_parts(cache, dev)
     shape = (n, tokens, hkv, 2 * half)
     for name, out in (("k_out", k_out), ("v_out", v_out)):
         if out is not None:
             _tensor(name, out, shape, torch.bfloat16, dev)
     with _Launch(dev, stream) as at:
-        results = []
-        for codes, scales, out in ((cache[0], cache[2], k_out), (cache[1], cache[3], v_out)):
-            if out is None:
-                out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-            desc = Fp4ValuesDesc(n, tokens, hkv, 2 * half, codes.stride()[:3], scales.stride()[:3])
-            _check(lib().simsd_fp4_values(ctypes.byref(desc), codes.data_ptr(), scales.data_ptr(),
-                                          out.data_ptr(), at.handle))
-            results.append(out)
-    return tuple(results)
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        desc = _fp4_values_desc(n, tokens, hkv, 2 * half, st[0], st[1], st[2])
+        _check(lib().simsd_fp4_values(ctypes.byref(desc), ctypes.byref(_fp4_pointers(cache, ss)),
+                                      k_out.data_ptr(), v_out.data_ptr(), at.handle))
+    return k_out, v_out
 
 
 @functools.lru_cache(maxsize=1024)

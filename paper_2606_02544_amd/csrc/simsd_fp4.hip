@@ -206,6 +206,11 @@ constexpr int kUnits = 4;        // of a thread
 
 template <typename Index>
 __global__ void __launch_bounds__(256) fp4_values_kernel(Fp4Args a) {
+  // Keys, then values (those that are wanted).
+  const bool value = !a.k_out || blockIdx.y == 1;
+  const uint8_t* codes = static_cast<const uint8_t*>(value ? a.v : a.k);
+  const uint8_t* scales = value ? a.v_scales : a.k_scales;
+  char* out = static_cast<char*>(value ? a.v_out : a.k_out);
   const Index per_row = a.groups * 4;
   const Index total = static_cast<Index>(a.rows) * per_row;
   const Index first = static_cast<Index>(blockIdx.x) * (256 * kUnits) + threadIdx.x;
@@ -218,14 +223,14 @@ __global__ void __launch_bounds__(256) fp4_values_kernel(Fp4Args a) {
     const int at = static_cast<int>(u - row * per_row);
     const Index r1 = row / a.n2;
     const int64_t i2 = row - r1 * a.n2, i0 = r1 / a.n1, i1 = r1 - i0 * a.n1;
-    w[i] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.codes) + i0 * a.c0 + i1 * a.c1 + i2 * a.c2 + at * 4);
-    s[i] = a.scales[i0 * a.s0 + i1 * a.s1 + i2 * a.s2 + at / 4];
+    w[i] = *reinterpret_cast<const uint32_t*>(codes + i0 * a.c0 + i1 * a.c1 + i2 * a.c2 + at * 4);
+    s[i] = scales[i0 * a.s0 + i1 * a.s1 + i2 * a.s2 + at / 4];
   }
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
     const Index u = first + i * 256;
     if (u >= total) break;
-    *reinterpret_cast<u32x4*>(static_cast<char*>(a.out) + static_cast<int64_t>(u) * 16) = fp4_values(w[i], s[i]);
+    *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(u) * 16) = fp4_values(w[i], s[i]);
   }
 }
 
@@ -243,10 +248,9 @@ hipError_t launch_fp4_append(const Fp4AppendArgs& f, bool interleaved, int cus, 
   return hipGetLastError();
 }
 
-hipError_t launch_fp4_values(const Fp4Args& a, int cus, hipStream_t st) {
-  (void)cus;
+hipError_t launch_fp4_values(const Fp4Args& a, hipStream_t st) {
   const int64_t units = a.rows * a.groups * 4;
-  const dim3 grid(static_cast<uint32_t>((units + 256 * kUnits - 1) / (256 * kUnits)));
+  const dim3 grid(static_cast<uint32_t>((units + 256 * kUnits - 1) / (256 * kUnits)), a.k_out && a.v_out ? 2 : 1);
   if (units < (int64_t{1} << 31) - 256 * kUnits) hipLaunchKernelGGL((fp4_values_kernel<int32_t>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((fp4_values_kernel<int64_t>), grid, dim3(256), 0, st, a);
   return hipGetLastError();

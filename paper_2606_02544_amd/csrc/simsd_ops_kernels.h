@@ -57,6 +57,7 @@ struct SpanArgs : ChunkArgs {
   const uint8_t* k_scales;      // 4-bit cache
   const uint8_t* v_scales;
   int64_t ss_seq, ss_tok, ss_head;
+  int scales_alike;             // strides of the codes: 16 times the scales', below 2^31
   const void* k_new;            // verification: kv_lens counts the cached prefix alone
   const void* v_new;
   const int32_t* step_map;
@@ -69,14 +70,17 @@ hipError_t launch_fp4(const SpanPlan& p, int d, const SpanArgs& a, hipStream_t s
 hipError_t launch_verify_span(const SpanPlan& p, bool fp4, int d, const SpanArgs& a, hipStream_t stream);
 
 struct Fp4Args {
-  const void* codes;            // [n0, n1, n2, d / 2]
-  const uint8_t* scales;        // [n0, n1, n2, d / 32]
-  void* out;
+  const void* k;                // codes [n0, n1, n2, d / 2]
+  const void* v;
+  const uint8_t* k_scales;      // [n0, n1, n2, d / 32]
+  const uint8_t* v_scales;
+  void* k_out;                  // each may be null
+  void* v_out;
   int64_t c0, c1, c2, s0, s1, s2;
   int64_t rows;                 // n0 * n1 * n2
   int n1, n2, groups;
 };
-hipError_t launch_fp4_values(const Fp4Args& a, int cus, hipStream_t stream);
+hipError_t launch_fp4_values(const Fp4Args& a, hipStream_t stream);
 
 // The append to a 4-bit cache.  `r` is the append of the queries alone (no KV heads), with
 // the keys and values and, in k_out and v_out, the cache's codes.

@@ -33,8 +33,8 @@ struct SpanBlock : Block {
   int t0, nt;                    // tiles [t0, t0 + nt) of the list are this work-group's
 };
 
-// How many key ranges the rows [row0, last] are divided into; VERIFY: the tile of the
-// new slots is the last of the list.
+// How many key ranges a list is divided into.  VERIFY: the tile of the new slots is the
+// last of the list.
 template <bool VERIFY>
 __device__ __attribute__((always_inline)) inline int ranges_of(const SpanArgs& a, int tiles, int TK) {
   const int c = a.chunk / TK;

@@ -45,7 +45,7 @@ static void set_plan(const SpanPlan& p, int page_size, int max_pages, const int3
   a->scale_log2 = p.scale_log2;
 }
 
-static void set_fp4(const simsd_fp4_cache* c, SpanArgs* a) {
+static void set_fp4(const simsd_fp4_cache* c, int64_t seq, int64_t tok, SpanArgs* a) {
   a->k_cache = c->k;
   a->v_cache = c->v;
   a->k_scales = static_cast<const uint8_t*>(c->k_scales);
@@ -53,6 +53,8 @@ static void set_fp4(const simsd_fp4_cache* c, SpanArgs* a) {
   a->ss_seq = c->scale_stride_seq;
   a->ss_tok = c->scale_stride_token;
   a->ss_head = c->scale_stride_head;
+  a->scales_alike = seq == 16 * c->scale_stride_seq && tok == 16 * c->scale_stride_token && seq < (int64_t{1} << 31) &&
+                    tok < (int64_t{1} << 31);
 }
 
 // ----------------------------------------------------------------------------
@@ -81,7 +83,7 @@ static simsd_status chunk_span(const char* op, const simsd_chunk_desc* desc, int
   if (st == SIMSD_OK && !fp4 && p.window == 0)   // (it reaches past every cache)
     return simsd_chunk_attention(desc, q, k_cache, v_cache, block_table, q_starts, kv_lens, out, lse, workspace,
                                  workspace_bytes, stream);
-  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->num_tokens > 0 ? desc->max_kv_len : 0);
+  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->num_tokens > 0 ? desc->max_kv_len : 0, desc->head_dim);
   if (st == SIMSD_OK) {
     ChunkPlan none;                // (the workspace is this plan's)
     st = check_chunk_args(desc, none, q, fp4 ? cache->k : k_cache, fp4 ? cache->v : v_cache, block_table, q_starts, kv_lens,
@@ -95,7 +97,7 @@ static simsd_status chunk_span(const char* op, const simsd_chunk_desc* desc, int
   a.q = q;
   a.k_cache = k_cache;
   a.v_cache = v_cache;
-  if (fp4) set_fp4(cache, &a);
+  if (fp4) set_fp4(cache, desc->cache_stride_seq, desc->cache_stride_token, &a);
   a.q_starts = q_starts;
   a.kv_lens = kv_lens;
   a.out = out;
@@ -169,7 +171,7 @@ static simsd_status verify_span(const char* op, const simsd_attn_desc* desc, int
   const hipError_t qe = stream_device(stream, &dev, &cus);
   SpanPlan p;
   simsd_status st = plan_verify_span(desc, fp4, window, sinks, cus, &p);
-  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->max_prefix_len);
+  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->max_prefix_len, desc->head_dim);
   if (st == SIMSD_OK) {
     AttnPlan none;                 // (the workspace is this plan's)
     st = check_attention_args(desc, none, q, k_new, v_new, fp4 ? cache->k : k_cache, fp4 ? cache->v : v_cache, block_table,
@@ -189,7 +191,7 @@ static simsd_status verify_span(const char* op, const simsd_attn_desc* desc, int
   a.v_new = v_new;
   a.k_cache = k_cache;
   a.v_cache = v_cache;
-  if (fp4) set_fp4(cache, &a);
+  if (fp4) set_fp4(cache, desc->cache_stride_seq, desc->cache_stride_token, &a);
   a.kv_lens = prefix_lens;
   a.step_map = step_map;
   a.num_ref = num_ref;
@@ -316,30 +318,33 @@ extern "C" simsd_status simsd_rotary_append_fp4(const simsd_rotary_desc* desc, c
   }
 }
 
-extern "C" simsd_status simsd_fp4_values(const simsd_fp4_values_desc* desc, const void* codes, const void* scales, void* out,
-                                         void* stream) {
+extern "C" simsd_status simsd_fp4_values(const simsd_fp4_values_desc* desc, const simsd_fp4_cache* cache, void* k_out,
+                                         void* v_out, void* stream) {
   try {
-    const simsd_status st = check_fp4_values(desc, codes, scales, out);
+    const simsd_status st = check_fp4_values(desc, cache, k_out, v_out);
     if (st != SIMSD_OK) return st;
     Fp4Args a{};
-    a.rows = desc->n0 * desc->n1 * desc->n2;
+    a.rows = int64_t{desc->num} * desc->tokens * desc->num_kv_heads;
     if (a.rows == 0) return SIMSD_OK;
     int dev = 0, cus = 0;
     const hipError_t qe = stream_device(stream, &dev, &cus);
     if (qe != hipSuccess) return hip_fail(qe, "simsd_fp4_values: device query");
-    a.codes = codes;
-    a.scales = static_cast<const uint8_t*>(scales);
-    a.out = out;
-    a.c0 = desc->code_stride[0];
-    a.c1 = desc->code_stride[1];
-    a.c2 = desc->code_stride[2];
-    a.s0 = desc->scale_stride[0];
-    a.s1 = desc->scale_stride[1];
-    a.s2 = desc->scale_stride[2];
-    a.n1 = desc->n1;
-    a.n2 = desc->n2;
+    a.k = cache->k;
+    a.v = cache->v;
+    a.k_scales = static_cast<const uint8_t*>(cache->k_scales);
+    a.v_scales = static_cast<const uint8_t*>(cache->v_scales);
+    a.k_out = k_out;
+    a.v_out = v_out;
+    a.c0 = desc->cache_stride_seq;
+    a.c1 = desc->cache_stride_token;
+    a.c2 = desc->cache_stride_head;
+    a.s0 = cache->scale_stride_seq;
+    a.s1 = cache->scale_stride_token;
+    a.s2 = cache->scale_stride_head;
+    a.n1 = desc->tokens;
+    a.n2 = desc->num_kv_heads;
     a.groups = desc->head_dim / 32;
-    const hipError_t e = launch_fp4_values(a, cus, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_fp4_values(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SIMSD_OK : hip_fail(e, "simsd_fp4_values launch");
   } catch (...) {
     return internal_error("simsd_fp4_values");

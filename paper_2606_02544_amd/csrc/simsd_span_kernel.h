@@ -411,10 +411,12 @@ __global__ void __launch_bounds__(RW * KW * 64, 2) span_bf16_kernel(SpanArgs a) 
 
 template <int D, bool PAGED, bool FP4, bool VERIFY>
 void launch_span_bf16(const SpanPlan& p, dim3 grid, const SpanArgs& a, hipStream_t st) {
-  switch (p.row_waves) {
-    case 2: hipLaunchKernelGGL((span_bf16_kernel<D, 2, 2, PAGED, FP4, VERIFY>), grid, dim3(256), 0, st, a); break;
-    case 4: hipLaunchKernelGGL((span_bf16_kernel<D, 4, 1, PAGED, FP4, VERIFY>), grid, dim3(256), 0, st, a); break;
-    default: hipLaunchKernelGGL((span_bf16_kernel<D, 8, 1, PAGED, FP4, VERIFY>), grid, dim3(512), 0, st, a); break;
+  if (p.row_waves == 4) {
+    hipLaunchKernelGGL((span_bf16_kernel<D, 4, 1, PAGED, FP4, VERIFY>), grid, dim3(256), 0, st, a);
+  } else if (p.row_waves == 8) {
+    hipLaunchKernelGGL((span_bf16_kernel<D, 8, 1, PAGED, FP4, VERIFY>), grid, dim3(512), 0, st, a);
+  } else if constexpr (!FP4) {                 // (4 bits: fp4_rows_kernel)
+    hipLaunchKernelGGL((span_bf16_kernel<D, 2, 2, PAGED, FP4, VERIFY>), grid, dim3(256), 0, st, a);
   }
 }
 

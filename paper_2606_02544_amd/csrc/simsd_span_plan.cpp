@@ -53,16 +53,16 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   if (c.window > c.max_kv) c.window = c.sinks = 0;
   r.window = c.window;
   r.sinks = c.sinks;
-  const int64_t TK = c.bf16 ? kTile : kTile / 2;
   int64_t most = int64_t{1} << 30;
   if (c.page_size > 0)   // a work-group holds the ids of its pages in LDS: two parts, each with an end page at either side
     most = std::max<int64_t>(int64_t{kMaxChunkPages - 4} * c.page_size / kTile * kTile, kTile);
   // Rows per work-group and key ranges per row: the cheapest by the estimate that the
   // chunk attention's plan makes (see there), over the tiles of a list.
-  struct Shape { int row_waves, rows, per_cu; double alone, full; };
-  constexpr Shape kBf16[] = {{2, 64, 2, 0.95, 1.35}, {4, 128, 2, 1.4, 2.2}, {8, 256, 1, 1.8, 2.1}};
-  constexpr Shape kF32[] = {{4, 16, 2, 2.0, 3.25}, {4, 32, 2, 3.5, 5.1}, {4, 64, 2, 5.8, 8.2}, {4, 128, 2, 10.4, 17.4}};
-  const Shape* shapes = c.bf16 ? kBf16 : kF32;
+  struct Shape { int row_waves, few, tile, rows, per_cu; double alone, full; };
+  constexpr Shape kBf16[] = {{2, 0, 64, 64, 2, 0.95, 1.6}, {4, 0, 64, 128, 2, 1.4, 2.2}, {8, 0, 64, 256, 1, 1.8, 2.1}};
+  constexpr Shape kFp4[] = {{0, 1, 32, 32, 3, 0.5, 1.2}, {0, 2, 32, 64, 2, 0.75, 1.3}, {4, 0, 64, 128, 2, 1.6, 2.4}, {8, 0, 64, 256, 1, 1.9, 2.1}};
+  constexpr Shape kF32[] = {{4, 0, 32, 16, 2, 2.0, 2.8}, {4, 0, 32, 32, 2, 3.2, 4.2}, {4, 0, 32, 64, 2, 7.0, 10.0}, {4, 0, 32, 128, 2, 13.0, 21.0}};
+  const Shape* shapes = c.fp4 ? kFp4 : c.bf16 ? kBf16 : kF32;
   const double scale_d = c.d / 128.0;
   const double key_bytes = 2.0 * (c.fp4 ? c.d * 17.0 / 32.0 : c.bf16 ? 2.0 * c.d : 4.0 * c.d);
   const bool open = c.window == 0 || c.window >= c.max_q;   // the lengths matter to the rows' keys
@@ -74,10 +74,10 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   int64_t chunk = 0;
   int per_cu = 1;
   double best = -1.0;
-  for (int i = 0; i < (c.bf16 ? 3 : 4); ++i) {
+  for (int i = 0; i < (c.bf16 && !c.fp4 ? 3 : 4); ++i) {
     const Shape& sh = shapes[i];
     if (i > 0 && shapes[i - 1].rows >= rows) break;   // no sequence fills more than the smaller one
-    const int64_t tiles = std::max<int64_t>(ceil_div(list_tiles(c, sh.rows, r.group, TK) * TK, kTile), 1);
+    const int64_t tiles = std::max<int64_t>(ceil_div(list_tiles(c, sh.rows, r.group, sh.tile) * sh.tile, kTile), 1);
     const double slots = static_cast<double>(sh.per_cu) * cus;
     const double filled = static_cast<double>(c.tokens) * r.group / c.batch / sh.rows;
     const double blocks = c.n_new > 0 ? std::ceil(filled) : c.batch > 1 ? std::max(filled + 0.5, 1.0) : std::ceil(filled);
@@ -85,7 +85,7 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
     for (int64_t s = 1; s <= std::min<int64_t>(tiles, 64); s += s < 8 ? 1 : s < 16 ? 2 : s < 32 ? 4 : 8) {
       const int64_t t = ceil_div(tiles, s);
       const double x = groups * s / slots;
-      const double cu = x <= 0.5 ? sh.alone : x <= 1.0 ? 0.5 * (sh.alone + sh.full) : sh.full;
+      const double cu = x <= 0.5 ? sh.alone : x <= 1.0 ? sh.alone + (sh.full - sh.alone) * (2.0 * x - 1.0) : sh.full;
       const double memory = kTile * key_bytes * std::min(x, 1.0) * slots / 5.5e6 / std::min(blocks, 8.0);
       const double one = t * std::max(cu * scale_d, memory);
       double us = x <= 1.0 ? one + 7.0 : even * x * (one + 5.0) + 0.35 * (one + 7.0);
@@ -94,6 +94,8 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
         best = us;
         chunk = t * kTile;
         r.row_waves = sh.row_waves;
+        r.few = sh.few;
+        r.tile = sh.tile;
         r.rows_pb = sh.rows;
         per_cu = sh.per_cu;
       }
@@ -102,7 +104,7 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   if (c.kv_chunk > 0) chunk = c.kv_chunk;
   chunk = std::min(chunk, most);
   r.chunk = static_cast<int>(chunk);
-  const int64_t splits = std::max<int64_t>(1, ceil_div(list_tiles(c, r.rows_pb, r.group, TK) * TK, chunk));
+  const int64_t splits = std::max<int64_t>(1, ceil_div(list_tiles(c, r.rows_pb, r.group, r.tile) * r.tile, chunk));
   if (splits > 65535) return fail(SIMSD_ERR_BAD_SHAPE, std::string(op) + ": too many key ranges");
   r.splits = static_cast<int>(splits);
   int64_t blocks;
@@ -233,15 +235,19 @@ simsd_status check_span_workspace(const char* op, const SpanPlan& p, const void*
   return SIMSD_OK;
 }
 
-simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len) {
+simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len, int head_dim) {
   if (!c) return fail(SIMSD_ERR_NULL_POINTER, std::string(op) + ": cache is NULL");
   if (max_len > 0 && (!c->k || !c->v || !c->k_scales || !c->v_scales))
     return fail(SIMSD_ERR_NULL_POINTER, std::string(op) + ": the cache's codes and scales are required");
   if (!aligned(c->k, 16) || !aligned(c->v, 16))
     return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": the cache's codes must be 16-byte aligned");
+  const int n = head_dim / 32;                   // (the attentions read a head's scales as a word)
+  if (reinterpret_cast<uintptr_t>(c->k_scales) % n != 0 || reinterpret_cast<uintptr_t>(c->v_scales) % n != 0)
+    return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": the cache's scales must be aligned to head_dim / 32 bytes");
   for (int64_t s : {c->scale_stride_seq, c->scale_stride_token, c->scale_stride_head}) {
     if (s < 0) return fail(SIMSD_ERR_BAD_SHAPE, std::string(op) + ": negative stride of the scales");
     if (s > (int64_t{1} << 48)) return fail(SIMSD_ERR_BAD_SHAPE, std::string(op) + ": stride of the scales beyond 2^48 bytes");
+    if (s % n != 0) return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": strides of the scales must be multiples of head_dim / 32");
   }
   return SIMSD_OK;
 }
@@ -262,7 +268,7 @@ simsd_status plan_fp4_append(const simsd_rotary_desc* d, const simsd_fp4_cache* 
   if (d->head_dim != 64 && d->head_dim != 128)
     return fail(SIMSD_ERR_UNSUPPORTED, "rotary_append_fp4: head_dim must be 64 or 128");
   st = check_code_strides("rotary_append_fp4", d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head);
-  if (st == SIMSD_OK) st = check_fp4_cache("rotary_append_fp4", c, d->num_tokens > 0 ? d->max_kv_len : 0);
+  if (st == SIMSD_OK) st = check_fp4_cache("rotary_append_fp4", c, d->num_tokens > 0 ? d->max_kv_len : 0, d->head_dim);
   if (st != SIMSD_OK) return st;
   const int64_t tokens = d->page_size > 0 ? d->page_size : d->max_kv_len;
   if (!apart(tokens, d->num_kv_heads, d->cache_stride_token, d->cache_stride_head, d->head_dim / 2) ||
@@ -271,24 +277,25 @@ simsd_status plan_fp4_append(const simsd_rotary_desc* d, const simsd_fp4_cache* 
   return SIMSD_OK;
 }
 
-simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const void* codes, const void* scales, const void* out) {
+simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const simsd_fp4_cache* c, const void* k_out, const void* v_out) {
   if (!d) return fail(SIMSD_ERR_NULL_POINTER, "fp4_values: descriptor is NULL");
-  if (d->n0 < 0 || d->n0 > INT32_MAX || d->n1 < 0 || d->n2 < 0)
-    return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: need n0 in [0, 2^31 - 1], n1 >= 0 and n2 >= 0");
-  if (static_cast<__int128>(d->n0) * d->n1 * d->n2 > (int64_t{1} << 36))
-    return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: n0 * n1 * n2 must be <= 2^36");
+  if (d->num < 0 || d->tokens < 0 || d->num_kv_heads < 0)
+    return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: need num, tokens and num_kv_heads >= 0");
+  if (static_cast<__int128>(d->num) * d->tokens * d->num_kv_heads > (int64_t{1} << 36))
+    return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: num * tokens * num_kv_heads must be <= 2^36");
   if (d->head_dim < 32 || d->head_dim > 512 || d->head_dim % 32 != 0)
     return fail(SIMSD_ERR_UNSUPPORTED, "fp4_values: head_dim must be a multiple of 32 in [32, 512]");
-  for (int i = 0; i < 3; ++i) {
-    if (d->code_stride[i] < 0 || d->scale_stride[i] < 0) return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: negative stride");
-    if (d->code_stride[i] > (int64_t{1} << 48) || d->scale_stride[i] > (int64_t{1} << 48))
-      return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: stride beyond 2^48 bytes");
-    if (d->code_stride[i] % 4 != 0) return fail(SIMSD_ERR_ALIGNMENT, "fp4_values: code strides must be multiples of 4");
+  for (int64_t s : {d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head}) {
+    if (s < 0) return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: negative stride");
+    if (s > (int64_t{1} << 48)) return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: stride beyond 2^48 bytes");
   }
-  if (d->n0 == 0 || d->n1 == 0 || d->n2 == 0) return SIMSD_OK;
-  if (!codes || !scales || !out) return fail(SIMSD_ERR_NULL_POINTER, "fp4_values: codes, scales and out are required");
-  if (!aligned(codes, 4) || !aligned(out, 16))
-    return fail(SIMSD_ERR_ALIGNMENT, "fp4_values: codes must be 4-byte and out 16-byte aligned");
+  simsd_status st = check_code_strides("fp4_values", d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head);
+  const bool some = d->num > 0 && d->tokens > 0 && d->num_kv_heads > 0;
+  if (st == SIMSD_OK) st = check_fp4_cache("fp4_values", c, some, d->head_dim);
+  if (st != SIMSD_OK || !some) return st;
+  if (!k_out && !v_out) return fail(SIMSD_ERR_NULL_POINTER, "fp4_values: k_out or v_out is required");
+  if (!aligned(k_out, 16) || !aligned(v_out, 16))
+    return fail(SIMSD_ERR_ALIGNMENT, "fp4_values: k_out and v_out must be 16-byte aligned");
   return SIMSD_OK;
 }
 

@@ -13,6 +13,8 @@ namespace simsd {
 struct SpanPlan {
   int group = 0;        // Hq / Hkv
   int row_waves = 0;    // bf16: waves that own distinct rows (32 each)
+  int few = 0;          // 4 bits, few rows: 32-row blocks that every wave holds (then no row waves)
+  int tile = 0;         // keys of a tile of the list
   int rows_pb = 0;      // rows per work-group
   int seq_blocks = 0;   // verification: row blocks of a sequence
   int blocks = 0;       // row-block numbers
@@ -33,10 +35,11 @@ simsd_status plan_verify_span(const simsd_attn_desc* d, bool fp4, int window, in
 
 // The workspace of a call with this plan.
 simsd_status check_span_workspace(const char* op, const SpanPlan& p, const void* workspace, size_t workspace_bytes);
-// The pointers and strides of a 4-bit cache of `max_len` tokens at most.
-simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len);
+// The pointers and strides of a 4-bit cache of `max_len` tokens at most (whose codes'
+// strides are the descriptor's).
+simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len, int head_dim);
 
 simsd_status plan_fp4_append(const simsd_rotary_desc* d, const simsd_fp4_cache* c);
-simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const void* codes, const void* scales, const void* out);
+simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const simsd_fp4_cache* c, const void* k_out, const void* v_out);
 
 }  // namespace simsd

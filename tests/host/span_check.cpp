@@ -158,7 +158,9 @@ static void common(const SpanPlan& p, bool bf16, int page_size, int64_t tokens, 
   if (page_size > 0) EXPECT(int64_t{p.chunk} / page_size + 4 <= kMaxChunkPages);
   EXPECT(int64_t{p.blocks} * hkv <= (1 << 22));
   EXPECT(p.fold == 0 || (p.splits == 1 && p.fold < p.blocks && p.blocks <= 2 * p.fold));
-  EXPECT(bf16 ? p.rows_pb == 32 * p.row_waves && (p.row_waves == 2 || p.row_waves == 4 || p.row_waves == 8)
+  EXPECT(p.tile == (bf16 && !p.few ? 64 : 32) && p.chunk % p.tile == 0);
+  EXPECT(p.few    ? bf16 && p.rows_pb == 32 * p.few && p.few <= 2 && p.row_waves == 0
+         : bf16   ? p.rows_pb == 32 * p.row_waves && (p.row_waves == 2 || p.row_waves == 4 || p.row_waves == 8)
               : p.rows_pb == 16 || p.rows_pb == 32 || p.rows_pb == 64 || p.rows_pb == 128);
   EXPECT(p.window >= 0 && p.sinks >= 0 && (p.window > 0 || p.sinks == 0));
   const size_t n = size_t(p.splits) * tokens * hq;
@@ -195,7 +197,8 @@ static int fuzz_chunk() {
   const bool bf16 = d.dtype == SIMSD_BF16;
   common(p, bf16, d.page_size, d.num_tokens, d.num_q_heads, d.num_kv_heads, d.head_dim);
   EXPECT(p.blocks == std::max<int64_t>(int64_t{d.num_tokens} * p.group - 1, 0) / p.rows_pb + d.batch);
-  covered(p, bf16 ? 64 : 32, d.max_kv_len, d.mask_block, p.window, p.sinks, false);
+  EXPECT(fp4 ? p.row_waves != 2 : p.few == 0);
+  covered(p, p.tile, d.max_kv_len, d.mask_block, p.window, p.sinks, false);
   return 1;
 }
 
@@ -225,7 +228,7 @@ static int fuzz_verify() {
   const int n = d.block_size + d.max_ref;
   common(p, true, d.page_size, int64_t{d.batch} * n, d.num_q_heads, d.num_kv_heads, d.head_dim);
   EXPECT(p.seq_blocks * p.rows_pb >= n * p.group && p.blocks == d.batch * p.seq_blocks);
-  covered(p, 64, d.max_prefix_len, 1, p.window, p.sinks, true);
+  covered(p, p.tile, d.max_prefix_len, 1, p.window, p.sinks, true);
   return 1;
 }
 
@@ -250,22 +253,21 @@ static void fuzz_append() {
   some_dtype(&d.dtype);
   simsd_fp4_cache c{};
   c.k = c.v = reinterpret_cast<void*>(uintptr_t{0x10000});
-  c.k_scales = c.v_scales = reinterpret_cast<void*>(uintptr_t{0x10001});
+  c.k_scales = c.v_scales = reinterpret_cast<void*>(uintptr_t{0x10004});
   c.scale_stride_seq = some_stride();
   c.scale_stride_token = some_stride();
   c.scale_stride_head = some_stride();
   if (plan_fp4_append(&d, rng() % 8 ? &c : nullptr) == SIMSD_OK) EXPECT(d.dtype == SIMSD_BF16 && d.cache_stride_head % 16 == 0);
   simsd_fp4_values_desc v{};
-  v.n0 = rng() % 4 ? some_int({0, 1, 100}) : some_stride();
-  v.n1 = some_int({1, 16});
-  v.n2 = some_int({1, 8});
-  v.head_dim = some_int({32, 64, 128});
-  for (int i = 0; i < 3; ++i) {
-    v.code_stride[i] = some_stride();
-    v.scale_stride[i] = some_stride();
-  }
-  if (check_fp4_values(&v, c.k, c.k_scales, c.k) == SIMSD_OK)
-    EXPECT(v.n0 >= 0 && v.n1 >= 0 && v.n2 >= 0 && v.n0 * v.n1 <= (int64_t{1} << 62) / std::max(v.n2, 1));
+  v.num = some_int({0, 1, 100});
+  v.tokens = some_int({1, 16});
+  v.num_kv_heads = some_int({1, 8});
+  v.head_dim = some_int({32, 64, 96, 128, 512});
+  v.cache_stride_seq = some_stride();
+  v.cache_stride_token = some_stride();
+  v.cache_stride_head = some_stride();
+  if (check_fp4_values(&v, rng() % 8 ? &c : nullptr, c.k, rng() % 2 ? c.v : nullptr) == SIMSD_OK)
+    EXPECT(v.num >= 0 && v.tokens >= 0 && v.num_kv_heads >= 0 && v.head_dim % 32 == 0 && v.head_dim <= 512);
 }
 
 int main() {

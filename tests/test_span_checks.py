@@ -42,7 +42,7 @@ def test_descriptor_layouts(tmp_path):
 
 
 def pointers(**kw):
-    d = dict(k=0x10000, v=0x10000, k_scales=0x10001, v_scales=0x10001, scale_stride_seq=512, scale_stride_token=4,
+    d = dict(k=0x10000, v=0x10000, k_scales=0x10002, v_scales=0x10002, scale_stride_seq=512, scale_stride_token=4,
              scale_stride_head=2)
     d.update(kw)
     return Fp4Pointers(**d)
@@ -126,7 +126,9 @@ def test_pointers(no_gpu, form):
             assert chunk("fp4", c, 8, 2, pointers(**{n: 0})) == 1, n
             assert verify("fp4", v, 8, 2, pointers(**{n: 0})) == 1, n
         assert chunk("fp4", c, 8, 2, pointers(v=0x10008)) == 4
-        assert chunk("fp4", c, 8, 2, pointers(scale_stride_token=-1)) == 2
+        assert chunk("fp4", c, 8, 2, pointers(scale_stride_token=-2)) == 2
+        assert chunk("fp4", c, 8, 2, pointers(scale_stride_token=3)) == 4
+        assert verify("fp4", v, 8, 2, pointers(v_scales=0x10003)) == 4
         assert verify("fp4", v, 8, 2, pointers(scale_stride_head=2 ** 48 + 1)) == 2
     # a workspace that is missing or short
     assert chunk(form, chunk_desc(kv_chunk=64, max_kv_len=640), 640, 0, workspace=NULL) == 5
@@ -158,26 +160,28 @@ def test_append(no_gpu):
     # rows of codes (32 bytes a head) or of scales (2) that overlap
     assert fp4_append(rotary_desc(cache_stride_head=16)) == 2
     assert fp4_append(rotary_desc(cache_stride_token=32)) == 2
-    assert fp4_append(d, pointers(scale_stride_head=1)) == 2 and fp4_append(d, pointers(scale_stride_token=2)) == 2
+    assert fp4_append(d, pointers(scale_stride_head=0)) == 2 and fp4_append(d, pointers(scale_stride_token=2)) == 2
+    assert fp4_append(d, pointers(k_scales=0x10001)) == 4 and fp4_append(d, pointers(scale_stride_seq=513)) == 4
     assert fp4_append(d, pointers(scale_stride_head=64, scale_stride_token=2), k=NULL) == 1     # (apart: tokens inside heads)
     assert fp4_append(rotary_desc(num_tokens=0), k=NULL, v=NULL) == 0
 
 
 def test_values(no_gpu):
-    def run(codes=FAKE, scales=FAKE, out=FAKE, **kw):
-        d = dict(n0=2, n1=3, n2=4, head_dim=64, code_stride=(384, 128, 32), scale_stride=(24, 8, 2))
+    def run(cache=Fp4Pointers, k_out=FAKE, v_out=FAKE, **kw):
+        d = dict(num=2, tokens=3, num_kv_heads=4, head_dim=64, cache_stride_seq=384, cache_stride_token=128, cache_stride_head=32)
         d.update(kw)
-        d["code_stride"], d["scale_stride"] = ((ctypes.c_int64 * 3)(*d[n]) for n in ("code_stride", "scale_stride"))
-        return binding.lib().simsd_fp4_values(ctypes.byref(Fp4ValuesDesc(**d)), codes, scales, out, None)
+        cache = cache and ctypes.byref(pointers() if cache is Fp4Pointers else cache)
+        return binding.lib().simsd_fp4_values(ctypes.byref(Fp4ValuesDesc(**d)), cache, k_out, v_out, None)
 
-    assert binding.lib().simsd_fp4_values(None, FAKE, FAKE, FAKE, None) == 1
-    for kw, status in ((dict(n0=-1), 2), (dict(n1=-1), 2), (dict(n0=2 ** 31), 2), (dict(n0=2 ** 20, n1=2 ** 16, n2=2), 2),
-                       (dict(head_dim=48), 3), (dict(head_dim=544), 3), (dict(code_stride=(384, 130, 32)), 4),
-                       (dict(scale_stride=(24, -8, 2)), 2), (dict(code_stride=(2 ** 49, 4, 4)), 2), (dict(codes=NULL), 1),
-                       (dict(scales=NULL), 1), (dict(out=NULL), 1), (dict(codes=ctypes.c_void_p(0x10002)), 4),
-                       (dict(out=ctypes.c_void_p(0x10008)), 4)):
+    assert binding.lib().simsd_fp4_values(None, None, FAKE, FAKE, None) == 1 and run(cache=NULL) == 1
+    for kw, status in ((dict(num=-1), 2), (dict(tokens=-1), 2), (dict(num_kv_heads=-2 ** 31), 2),
+                       (dict(num=2 ** 20, tokens=2 ** 16, num_kv_heads=2), 2), (dict(head_dim=48), 3), (dict(head_dim=544), 3),
+                       (dict(head_dim=0), 3), (dict(cache_stride_token=136), 4), (dict(cache_stride_seq=-16), 2),
+                       (dict(cache_stride_head=2 ** 49), 2), (dict(cache=pointers(k=0)), 1), (dict(cache=pointers(v_scales=0)), 1),
+                       (dict(k_out=NULL, v_out=NULL), 1), (dict(cache=pointers(k=0x10008)), 4),
+                       (dict(k_out=ctypes.c_void_p(0x10008)), 4), (dict(cache=pointers(scale_stride_seq=-2)), 2)):
         assert run(**kw) == status, kw
-    assert run(n0=0, codes=NULL) == 0 and run(n2=0) == 0
+    assert run(num=0, cache=pointers(k=0), k_out=NULL, v_out=NULL) == 0 and run(num_kv_heads=0) == 0
 
 
 # --- the binding ----------------------------------------------------------------
