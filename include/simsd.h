@@ -655,7 +655,7 @@ typedef struct {
 
 /*
  * The values of a cache's keys and of its values: k_out and v_out [num, tokens,
- * num_kv_heads, head_dim] bf16, 16-byte aligned, each or NULL.  Exact; past bf16's
+ * num_kv_heads, head_dim] bf16, 16-byte aligned, not the same, each or NULL.  Exact; past bf16's
  * range infinite (no append writes such).  One kernel.
  */
 simsd_status simsd_fp4_values(const simsd_fp4_values_desc* desc, const simsd_fp4_cache* cache,

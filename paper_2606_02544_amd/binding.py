@@ -1284,7 +1284,7 @@ def rotary_append_fp4(q, k, v, cache: Fp4Cache, block_table, q_starts, kv_lens, 
         if q is not None and q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         desc = _rotary_desc(T, hq, hkv, d, rot, int(bool(interleaved)), b, max_kv_len, page_size, pages,
-                            cache.k.shape[0] if pages else 0, float(attn_factor), qs[0], qs[1],
+                            cache[0].shape[0] if pages else 0, float(attn_factor), qs[0], qs[1],
                             ks[0], ks[1], vs[0], vs[1], qo[0], qo[1], 0, 0, cs[0], cs[1], cs[2],
                             _dtype_code(dt))
         _check(lib().simsd_rotary_append_fp4(

@@ -294,6 +294,7 @@ simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const simsd_fp4_ca
   if (st == SIMSD_OK) st = check_fp4_cache("fp4_values", c, some, d->head_dim);
   if (st != SIMSD_OK || !some) return st;
   if (!k_out && !v_out) return fail(SIMSD_ERR_NULL_POINTER, "fp4_values: k_out or v_out is required");
+  if (k_out == v_out) return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: k_out and v_out must not be the same");
   if (!aligned(k_out, 16) || !aligned(v_out, 16))
     return fail(SIMSD_ERR_ALIGNMENT, "fp4_values: k_out and v_out must be 16-byte aligned");
   return SIMSD_OK;

@@ -178,7 +178,7 @@ def test_values(no_gpu):
                        (dict(num=2 ** 20, tokens=2 ** 16, num_kv_heads=2), 2), (dict(head_dim=48), 3), (dict(head_dim=544), 3),
                        (dict(head_dim=0), 3), (dict(cache_stride_token=136), 4), (dict(cache_stride_seq=-16), 2),
                        (dict(cache_stride_head=2 ** 49), 2), (dict(cache=pointers(k=0)), 1), (dict(cache=pointers(v_scales=0)), 1),
-                       (dict(k_out=NULL, v_out=NULL), 1), (dict(cache=pointers(k=0x10008)), 4),
+                       (dict(k_out=NULL, v_out=NULL), 1), (dict(v_out=FAKE, k_out=FAKE), 2), (dict(cache=pointers(k=0x10008)), 4),
                        (dict(k_out=ctypes.c_void_p(0x10008)), 4), (dict(cache=pointers(scale_stride_seq=-2)), 2)):
         assert run(**kw) == status, kw
     assert run(num=0, cache=pointers(k=0), k_out=NULL, v_out=NULL) == 0 and run(num_kv_heads=0) == 0
