@@ -18,7 +18,13 @@ namespace {
 // (An fp32 rotation is off by 1e-7, which moves one key in ten million to the
 // next code: a step of up to a third.  The fp64 products hide behind the loads.)
 //
-// What bounds it: memory.  A head of 128 is read as 256 bytes and written as 68.
+// What bounds it: memory.  A head of 128 is read as 256 bytes and written as 68.  Of
+// 32768 tokens (32 query heads and 8 KV heads of 128, 709 MB) it reaches 3.8 TB/s in
+// 188 us, where a copy of as many bytes takes 146: the queries' part goes at 5, the keys'
+// and values' at about half of that, whose loads wait for the token's angles and cache
+// row and whose stores are 4 bytes a thread.  (The two parts in turn, eight work-groups
+// of each, so that one fills the other's waits: 0 to 3 % less there, 2 % more for 4200
+// ragged tokens.)
 // ----------------------------------------------------------------------------
 constexpr int kMaxHalf = 64;     // pairs of the largest head
 
@@ -200,7 +206,8 @@ void launch_append(const Fp4AppendArgs& f, int cus, hipStream_t st) {
 
 // ----------------------------------------------------------------------------
 // The values of codes in bf16: a thread takes eight dims (4 bytes in, 16 out), and
-// several of them a work-group's width apart.  Memory bounds it.
+// several of them a work-group's width apart.  Memory bounds it: 408 MB in 69 us, 6 TB/s
+// (the codes partly from the last-level cache, as written just before).
 // ----------------------------------------------------------------------------
 constexpr int kUnits = 4;        // of a thread
 

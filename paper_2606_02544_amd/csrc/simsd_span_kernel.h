@@ -7,6 +7,18 @@
 // rows, KW = 2: a second wave for the other 32 keys of each).  Tiles that some row does
 // not see whole take a word of visible keys a row and 32 keys: from its limit and first
 // key, or, for the tile of the new slots, the temporal mask's word.
+//
+// 4 bits: a tile's codes and scales are loaded into registers a tile ahead, and made bf16
+// on the way into LDS once for all row waves: two instructions a word of codes
+// (v_cvt_scalef32_pk_bf16_fp4), which is why this kernel takes 128 or 256 rows and
+// fewer go to simsd_fp4_rows.h.
+//
+// What bounds it: matrix cores and softmax in one chain.  32 query and 8 KV heads of 128:
+// two prompts of 8192 under a window of 2048 588 us (826 TFLOP/s; 410 at the rate of a
+// large product), the last 2048 tokens of four 16384 over 4 bits 1880 us (1098 TFLOP/s),
+// 64 slots of 16 sequences over a window of 4096 95 to 116 us (69 GFLOP, 290 MB) and 12 for
+// the join of its two ranges.  Single tokens are bound by HBM: 64 over a window of 4096
+// 188 us, 5.4 TB/s.
 #pragma once
 
 #include <type_traits>

@@ -57,7 +57,19 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   if (c.page_size > 0)   // a work-group holds the ids of its pages in LDS: two parts, each with an end page at either side
     most = std::max<int64_t>(int64_t{kMaxChunkPages - 4} * c.page_size / kTile * kTile, kTile);
   // Rows per work-group and key ranges per row: the cheapest by the estimate that the
-  // chunk attention's plan makes (see there), over the tiles of a list.
+  // chunk attention's plan makes (see there), over the tiles of a list.  alone, full: us of
+  // a work-group for 64 keys (heads of 128) where it has a unit to itself and where the
+  // units are full, from the difference of calls over 8192 and 16384 keys.
+  // Both sides of what it chooses, us on the GPU (32 query and 8 KV heads of 128, 4 bits):
+  //   64 verifications of 16 slots, prefixes of     planned  whole lists  16384  8192  4096
+  //     16640 each                                    391        367       376   378   411
+  //     512 to 32768, evenly                          439        484       456   434   430
+  //   43 of them, 24960 each                          401        442       417   423   418
+  //   16 of them, 512 to 32768                        162        387       212   160   166
+  //   64 single tokens over 512 to 32768              258        296       261   263   257
+  //   one over 32768                                   26        272       144    78    46
+  // and of the rows: 64 slots of 16 sequences over a window of 4096 in bf16, 256 rows in
+  // two ranges 127, 128 rows in two 127, 128 rows in one 129.
   struct Shape { int row_waves, few, tile, rows, per_cu; double alone, full; };
   constexpr Shape kBf16[] = {{2, 0, 64, 64, 2, 0.95, 1.6}, {4, 0, 64, 128, 2, 1.4, 2.2}, {8, 0, 64, 256, 1, 1.8, 2.1}};
   constexpr Shape kFp4[] = {{0, 1, 32, 32, 3, 0.5, 1.2}, {0, 2, 32, 64, 2, 0.75, 1.3}, {4, 0, 64, 128, 2, 1.6, 2.4}, {8, 0, 64, 256, 1, 1.9, 2.1}};
