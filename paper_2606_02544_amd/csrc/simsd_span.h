@@ -189,7 +189,9 @@ template <int D, bool BF16, bool VERIFY>
 void launch_span_merge(const SpanPlan& p, const SpanArgs& a, int TK, hipStream_t st) {
   if (p.splits == 1) return;
   constexpr int RPW = 64 / (D / 4);
-  const bool wide = p.splits > 4;
+  // WIDE where the chip holds all its work-groups at once (eight to a unit): in rounds of
+  // them their chains of loads add up (1024 rows of 32 heads: 28 us, with two rows to each wave 14).
+  const bool wide = p.splits > 4 && int64_t{a.tokens} * ((a.hq + RPW - 1) / RPW) <= 2048;
   const int per = wide ? RPW : 4 * RPW;
   const dim3 grid(a.tokens, (a.hq + per - 1) / per);
   if (wide) hipLaunchKernelGGL((span_merge_kernel<D, BF16, VERIFY, true>), grid, dim3(256), 0, st, a, TK);
