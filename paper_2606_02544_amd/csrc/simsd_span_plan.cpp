@@ -61,15 +61,20 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   // a work-group for 64 keys (heads of 128) where it has a unit to itself and where the
   // units are full, from the difference of calls over 8192 and 16384 keys.
   // Both sides of what it chooses, us on the GPU (32 query and 8 KV heads of 128, 4 bits):
-  //   64 verifications of 16 slots, prefixes of     planned  whole lists  16384  8192  4096
-  //     16640 each                                    391        367       376   378   411
-  //     512 to 32768, evenly                          439        484       456   434   430
-  //   43 of them, 24960 each                          401        442       417   423   418
-  //   16 of them, 512 to 32768                        162        387       212   160   166
-  //   64 single tokens over 512 to 32768              258        296       261   263   257
-  //   one over 32768                                   26        272       144    78    46
+  //   verifications of 16 slots, prefixes of          planned  ranges of 16384  8192  4096
+  //     64: 16640 each                                   397              380   388   412
+  //     64: 512 to 32768, evenly                         429              401   420   436
+  //     64: 4160, 12480, 20800 and 29120 in turn         401              385   396   432
+  //     43: 24960 each                                   416              409   418   415
+  //     16: 512 to 32768                                 146              211   163   160
+  //   64 single tokens over 512 to 32768                 263              268   263   257
+  //   one over 32768                                      26              143    78    46
   // and of the rows: 64 slots of 16 sequences over a window of 4096 in bf16, 256 rows in
   // two ranges 127, 128 rows in two 127, 128 rows in one 129.
+  // The end of a call, when some units have run out of work, counts less where lists of
+  // few rows start from the longest down: 0.1 of a work-group in place of 0.35 takes 8
+  // ragged verifications from 103 to 65, 16 of up to 8192 from 66 to 52, 32 from 232 to 221,
+  // and half of 8320 with half of 24960 from 403 to 437.
   struct Shape { int row_waves, few, tile, rows, per_cu; double alone, full; };
   constexpr Shape kBf16[] = {{2, 0, 64, 64, 2, 0.95, 1.6}, {4, 0, 64, 128, 2, 1.4, 2.2}, {8, 0, 64, 256, 1, 1.8, 2.1}};
   constexpr Shape kFp4[] = {{0, 1, 32, 32, 3, 0.5, 1.2}, {0, 2, 32, 64, 2, 0.75, 1.3}, {4, 0, 64, 128, 2, 1.6, 2.4}, {8, 0, 64, 256, 1, 1.9, 2.1}};
@@ -100,7 +105,8 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
       const double cu = x <= 0.5 ? sh.alone : x <= 1.0 ? sh.alone + (sh.full - sh.alone) * (2.0 * x - 1.0) : sh.full;
       const double memory = kTile * key_bytes * std::min(x, 1.0) * slots / 5.5e6 / std::min(blocks, 8.0);
       const double one = t * std::max(cu * scale_d, memory);
-      double us = x <= 1.0 ? one + 7.0 : even * x * (one + 5.0) + 0.35 * (one + 7.0);
+      const double end = sh.few > 0 && c.window == 0 && c.batch <= 64 ? 0.1 : 0.35;
+      double us = x <= 1.0 ? one + 7.0 : even * x * (one + 5.0) + end * (one + 7.0);
       if (s > 1) us += 5.0 + s * part_us;
       if (best < 0.0 || us < best) {
         best = us;
