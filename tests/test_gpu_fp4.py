@@ -409,6 +409,31 @@ def test_one_cache_for_all_sequences_and_no_keys():
     assert not bool(out.any()) and bool(torch.isneginf(lse).all())
 
 
+@pytest.mark.parametrize("hq,hkv", [(16, 1), (15, 1), (26, 2)])
+def test_blocks_that_end_inside_a_token(hq, hkv):
+    """Blocks that hold part of a token's heads."""
+    s = make([(1, 90), (9, 200), (1, 1), (30, 31)], hq, hkv, 64, 16, 12)
+    for kv_chunk in (0, 64):
+        check(s, *call(s, mask_block=1, kv_chunk=kv_chunk), 1)
+        check(s, *call(s, mask_block=1, kv_chunk=kv_chunk, window=40, sinks=2), 1, 40, 2)
+
+
+def test_no_rows_no_sequences_and_no_log_sum_exps():
+    from paper_2606_02544_amd import binding
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    c = binding.fp4_cache(2, 32, 2, 64)
+    none = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    out, lse = binding.chunk_attention_fp4(none, c, None, i32(0, 0, 0), i32(5, 7), max_q_len=1, max_kv_len=32)
+    assert out.shape == none.shape and lse.shape == (4, 0)
+    freq, _ = binding.rope_frequencies(64, 10000.0)
+    q = binding.rotary_append_fp4(none, none[:, :2], none[:, :2], c, None, i32(0, 0, 0), i32(5, 7), freq, max_kv_len=32)
+    assert q.shape == none.shape and not any(bool(x.any()) for x in c)
+    s = make([(3, 80), (1, 300)], 4, 2, 128, 16, 13)
+    for kv_chunk in (0, 64):
+        out, lse = call(s, mask_block=1, kv_chunk=kv_chunk, want_lse=False)
+        assert lse is None and torch.equal(out, call(s, mask_block=1, kv_chunk=kv_chunk)[0])
+
+
 def test_replays_of_two_graphs_threads_and_another_stream():
     import threading
     from paper_2606_02544_amd import binding

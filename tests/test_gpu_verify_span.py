@@ -157,6 +157,24 @@ def test_a_large_batch():
         check(s, *call(s, kv_chunk=kv_chunk, window=90, sinks=2), 90, 2)
 
 
+@pytest.mark.parametrize("page", [0, 16])
+def test_order_of_the_prefixes(page):
+    """Lengths that rise, fall, repeat and are 0: each sequence has its own outputs."""
+    for prefix in ([5, 300, 0, 64, 300, 17, 0], [700, 400, 100], [1, 2, 3, 500], list(range(64))):
+        s = make("fp4", prefix, 4, 2, 4, 2, 64, page, len(prefix))
+        for kv_chunk in (0, 128):
+            check(s, *call(s, kv_chunk=kv_chunk), 0, 0)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_blocks_that_end_inside_a_slot(form):
+    s = make(form, [90, 0, 200], 7, 4, 15, 1, 64, 16, 12)
+    for kv_chunk in (0, 64):
+        check(s, *call(s, kv_chunk=kv_chunk, window=70, sinks=2), 70, 2)
+        if form == "fp4":
+            check(s, *call(s, kv_chunk=kv_chunk), 0, 0)
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_replays_of_a_graph_and_another_stream(form):
     from paper_2606_02544_amd import binding
