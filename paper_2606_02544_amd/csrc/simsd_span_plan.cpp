@@ -75,9 +75,15 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   // few rows start from the longest down: 0.1 of a work-group in place of 0.35 takes 8
   // ragged verifications from 103 to 65, 16 of up to 8192 from 66 to 52, 32 from 232 to 221,
   // and half of 8320 with half of 24960 from 403 to 437.
+  // Chunks over 4 bits in blocks of 64, 128 and 256 rows: 11 prompts of up to 754 64, 45 and
+  // 48, 7 of up to 1243 110, 83 and 90, 24 chunks of up to 469 past 3000 tokens 400, 388
+  // and 407, 16 of 32 past 8000 103, 103 and 142, 42 verifications of 512 rows (heads of 64)
+  // 73, 52 and 60.  The estimate takes 48, 91, 388, 106 and 60: between blocks this near it
+  // errs both ways, and to make it prefer 128 throughout takes four prompts' last 2048 tokens
+  // of 16384 from 1939 to 2081.
   struct Shape { int row_waves, few, tile, rows, per_cu; double alone, full; };
   constexpr Shape kBf16[] = {{2, 0, 64, 64, 2, 0.95, 1.6}, {4, 0, 64, 128, 2, 1.4, 2.2}, {8, 0, 64, 256, 1, 1.8, 2.1}};
-  constexpr Shape kFp4[] = {{0, 1, 32, 32, 3, 0.5, 1.2}, {0, 2, 32, 64, 2, 0.75, 1.3}, {4, 0, 64, 128, 2, 1.6, 2.4}, {8, 0, 64, 256, 1, 1.9, 2.1}};
+  constexpr Shape kFp4[] = {{0, 1, 32, 32, 3, 0.5, 1.2}, {0, 2, 32, 64, 2, 0.75, 1.3}, {4, 0, 64, 128, 2, 1.4, 2.2}, {8, 0, 64, 256, 1, 1.9, 2.1}};
   constexpr Shape kF32[] = {{4, 0, 32, 16, 2, 2.0, 2.8}, {4, 0, 32, 32, 2, 3.2, 4.2}, {4, 0, 32, 64, 2, 7.0, 10.0}, {4, 0, 32, 128, 2, 13.0, 21.0}};
   const Shape* shapes = c.fp4 ? kFp4 : c.bf16 ? kBf16 : kF32;
   const double scale_d = c.d / 128.0;
@@ -106,7 +112,8 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
       const double memory = kTile * key_bytes * std::min(x, 1.0) * slots / 5.5e6 / std::min(blocks, 8.0);
       const double one = t * std::max(cu * scale_d, memory);
       const double end = sh.few > 0 && c.window == 0 && c.batch <= 64 ? 0.1 : 0.35;
-      double us = x <= 1.0 ? one + 7.0 : even * x * (one + 5.0) + end * (one + 7.0);
+      const double start = sh.few == 2 ? 7.0 : 5.0;
+      double us = x <= 1.0 ? one + 7.0 : even * x * (one + start) + end * (one + 7.0);
       if (s > 1) us += 5.0 + s * part_us;
       if (best < 0.0 || us < best) {
         best = us;
