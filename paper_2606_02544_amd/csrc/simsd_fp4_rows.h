@@ -17,7 +17,7 @@
 // Why waves on their own: with one tile of 64 keys shared by the row waves, as in
 // simsd_span_kernel.h, a tile's bytes are a quarter of bf16's and its two barriers are
 // not: 64 single tokens of uneven length (1.06 M keys, 8 KV heads of 128) took 421 us and
-// 64 verifications over as many 621; this kernel takes 256 to 288 and 418 to 453.
+// 64 verifications over as many 621; this kernel takes 256 to 288 and 400 to 453.
 //
 // What bounds it.  32 rows (12 waves a CU): HBM, 397 ns for 64 keys a CU, 5.4 TB/s; of
 // 262 us of a pass there 232 are that and the rest uneven ends and the start of a work-group (8 to

@@ -62,12 +62,12 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   // units are full, from the difference of calls over 8192 and 16384 keys.
   // Both sides of what it chooses, us on the GPU (32 query and 8 KV heads of 128, 4 bits):
   //   verifications of 16 slots, prefixes of          planned  ranges of 16384  8192  4096
-  //     64: 16640 each                                   397              380   388   412
-  //     64: 512 to 32768, evenly                         429              401   420   436
-  //     64: 4160, 12480, 20800 and 29120 in turn         401              385   396   432
-  //     43: 24960 each                                   416              409   418   415
-  //     16: 512 to 32768                                 146              211   163   160
-  //   64 single tokens over 512 to 32768                 263              268   263   257
+  //     64: 16640 each                                   395              380   388   412
+  //     64: 512 to 32768, evenly                         402              409   420   436
+  //     64: 4160, 12480, 20800 and 29120 in turn         409              385   396   432
+  //     43: 24960 each                                   410              417   418   415
+  //     16: 512 to 32768                                 147              211   163   160
+  //   64 single tokens over 512 to 32768                 262              268   263   257
   //   one over 32768                                      26              143    78    46
   // and of the rows: 64 slots of 16 sequences over a window of 4096 in bf16, 256 rows in
   // two ranges 127, 128 rows in two 127, 128 rows in one 129.
