@@ -6,8 +6,10 @@
 // block that is [0, sinks) and [lo, hi), lo being the first row's first key and hi the
 // last row's limit.  If the two meet, the list goes from key 0 (from lo without sinks)
 // to hi; otherwise it has tiles for the sinks, which every row sees whole, and then
-// those of [lo, hi).  Keys outside both parts are never read, nor are their pages: a
-// cache may have given them away.
+// those of [lo, hi), of which there are none if that is empty: a verification's slots see
+// no cached key by a window of one, lo = hi being the prefix's length.  Keys outside both
+// parts are never read, nor are their pages: a cache may have given them away, and the
+// key at hi may lie behind its end.
 #pragma once
 
 #include <algorithm>
@@ -57,7 +59,7 @@ SIMSD_LIST Span span_of(int all_sinks, int first, int hi, int TK) {
   s.sink_end = apart ? sinks : 0;
   s.sink_tiles = (s.sink_end + TK - 1) / TK;
   s.win0 = s.lo / TK * TK;
-  s.tiles = s.sink_tiles + (hi > s.win0 ? (hi - s.win0 + TK - 1) / TK : 0);
+  s.tiles = s.sink_tiles + (hi > s.lo ? (hi - s.win0 + TK - 1) / TK : 0);
   return s;
 }
 
