@@ -618,7 +618,8 @@ simsd_status simsd_rotary_append_fp4(const simsd_rotary_desc* desc, const void* 
 
 /*
  * simsd_chunk_attention_window over a 4-bit cache: its keys and values are the exact
- * values of their codes, and the arithmetic is that of bf16.  dtype (of q and out)
+ * values of their codes, past bf16's range (at scales of 253 and 254, which no append
+ * writes) infinite, and the arithmetic is that of bf16.  dtype (of q and out)
  * SIMSD_BF16 only (SIMSD_ERR_UNSUPPORTED); cache_stride_* in bytes, multiples of 16.
  */
 size_t simsd_chunk_attention_fp4_workspace_size(const simsd_chunk_desc* desc, int32_t window,

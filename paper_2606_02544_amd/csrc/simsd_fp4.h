@@ -23,6 +23,13 @@ __device__ inline u32x4 fp4_values(uint32_t w, uint32_t scale) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
 }
 
+// Eight codes without those that are past bf16's range at a scale of 254 (`shift` 0: from
+// 2 on at 2^127, the codes' bit 2) or 253 (1: 4 and 6 at 2^126, their bits 2 and 1).
+__device__ inline uint32_t fp4_finite(uint32_t w, uint32_t shift) {
+  const uint32_t past = w & (w << shift) & 0x44444444u;
+  return w & ~(past | (past - (past >> 2)));
+}
+
 // The scale byte of 32 values whose largest magnitude has these fp32 bits: the least
 // exponent at which it is below 7, which rounds to 6.  (Adding a quarter of the mantissa's
 // range carries into the exponent from 1.75 * 2^x = 7 * 2^(x - 2) on.)  255: one of them is

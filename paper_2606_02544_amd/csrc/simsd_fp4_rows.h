@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(256, RB == 1 ? 3 : 2) fp4_rows_kernel(SpanArgs
       }
   };
 
-  int bad_first = 0x7fffffff, bad_last = -1;   // masked tiles with values that are NaN
+  int bad_first = 0x7fffffff, bad_last = -1;   // masked tiles with values that are not finite
   for (int it = 0; it < items; ++it) {
     asm volatile("" : "+v"(put), "+v"(get[0]), "+v"(get[1]) :: "memory");
     const TileKeys k = list(it);
@@ -317,14 +317,17 @@ __global__ void __launch_bounds__(256, RB == 1 ? 3 : 2) fp4_rows_kernel(SpanArgs
     uint32_t ks[CH], vs[CH];
     split_scales(ks, vs);
     if (masked) {
-      bool mine = false;
+      bool mine = false;                       // (253 and 254 hold values past bf16's range, and others)
 #pragma unroll
-      for (int i = 0; i < CH; ++i)
-        if (vs[i] >= 253u) {                   // (253 and 254 hold values past bf16's range)
-          vs[i] = 0u;
-          mine = true;
-        }
+      for (int i = 0; i < CH; ++i) mine |= vs[i] >= 253u;
       if (__any(mine)) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+          if (vs[i] >= 253u) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vx[i][j] = fp4_finite(vx[i][j], vs[i] == 253u ? 1u : 0u);
+            if (vs[i] == 255u) vs[i] = 0u;
+          }
         bad_first = min(bad_first, it);
         bad_last = it;
       }
