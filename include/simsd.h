@@ -591,10 +591,12 @@ simsd_status simsd_verify_attention_window(const simsd_attn_desc* desc, int32_t 
 typedef struct {
   void* k;                    /* codes, 16-byte aligned                           */
   void* v;
-  void* k_scales;             /* scales, aligned to head_dim / 32 bytes           */
+  void* k_scales;             /* scales, aligned to head_dim / 32 bytes
+                                 (simsd_fp4_values: at any address)               */
   void* v_scales;
   int64_t scale_stride_seq;   /* bytes between sequences (contiguous) / pages; all
-                                 three are multiples of head_dim / 32             */
+                                 three are multiples of head_dim / 32
+                                 (simsd_fp4_values: any, >= 0)                    */
   int64_t scale_stride_token;
   int64_t scale_stride_head;
 } simsd_fp4_cache;

@@ -83,7 +83,7 @@ static simsd_status chunk_span(const char* op, const simsd_chunk_desc* desc, int
   if (st == SIMSD_OK && !fp4 && p.window == 0)   // (it reaches past every cache)
     return simsd_chunk_attention(desc, q, k_cache, v_cache, block_table, q_starts, kv_lens, out, lse, workspace,
                                  workspace_bytes, stream);
-  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->num_tokens > 0 ? desc->max_kv_len : 0, desc->head_dim);
+  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->num_tokens > 0 ? desc->max_kv_len : 0, desc->head_dim / 32);
   if (st == SIMSD_OK) {
     ChunkPlan none;                // (the workspace is this plan's)
     st = check_chunk_args(desc, none, q, fp4 ? cache->k : k_cache, fp4 ? cache->v : v_cache, block_table, q_starts, kv_lens,
@@ -171,7 +171,7 @@ static simsd_status verify_span(const char* op, const simsd_attn_desc* desc, int
   const hipError_t qe = stream_device(stream, &dev, &cus);
   SpanPlan p;
   simsd_status st = plan_verify_span(desc, fp4, window, sinks, cus, &p);
-  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->max_prefix_len, desc->head_dim);
+  if (st == SIMSD_OK && fp4) st = check_fp4_cache(op, cache, desc->max_prefix_len, desc->head_dim / 32);
   if (st == SIMSD_OK) {
     AttnPlan none;                 // (the workspace is this plan's)
     st = check_attention_args(desc, none, q, k_new, v_new, fp4 ? cache->k : k_cache, fp4 ? cache->v : v_cache, block_table,

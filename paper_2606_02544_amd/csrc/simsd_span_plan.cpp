@@ -260,19 +260,18 @@ simsd_status check_span_workspace(const char* op, const SpanPlan& p, const void*
   return SIMSD_OK;
 }
 
-simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len, int head_dim) {
+simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len, int scales_to) {
   if (!c) return fail(SIMSD_ERR_NULL_POINTER, std::string(op) + ": cache is NULL");
   if (max_len > 0 && (!c->k || !c->v || !c->k_scales || !c->v_scales))
     return fail(SIMSD_ERR_NULL_POINTER, std::string(op) + ": the cache's codes and scales are required");
   if (!aligned(c->k, 16) || !aligned(c->v, 16))
     return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": the cache's codes must be 16-byte aligned");
-  const int n = head_dim / 32;                   // (the attentions read a head's scales as a word)
-  if (reinterpret_cast<uintptr_t>(c->k_scales) % n != 0 || reinterpret_cast<uintptr_t>(c->v_scales) % n != 0)
+  if (!aligned(c->k_scales, scales_to) || !aligned(c->v_scales, scales_to))
     return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": the cache's scales must be aligned to head_dim / 32 bytes");
   for (int64_t s : {c->scale_stride_seq, c->scale_stride_token, c->scale_stride_head}) {
     if (s < 0) return fail(SIMSD_ERR_BAD_SHAPE, std::string(op) + ": negative stride of the scales");
     if (s > (int64_t{1} << 48)) return fail(SIMSD_ERR_BAD_SHAPE, std::string(op) + ": stride of the scales beyond 2^48 bytes");
-    if (s % n != 0) return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": strides of the scales must be multiples of head_dim / 32");
+    if (s % scales_to != 0) return fail(SIMSD_ERR_ALIGNMENT, std::string(op) + ": strides of the scales must be multiples of head_dim / 32");
   }
   return SIMSD_OK;
 }
@@ -293,7 +292,7 @@ simsd_status plan_fp4_append(const simsd_rotary_desc* d, const simsd_fp4_cache* 
   if (d->head_dim != 64 && d->head_dim != 128)
     return fail(SIMSD_ERR_UNSUPPORTED, "rotary_append_fp4: head_dim must be 64 or 128");
   st = check_code_strides("rotary_append_fp4", d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head);
-  if (st == SIMSD_OK) st = check_fp4_cache("rotary_append_fp4", c, d->num_tokens > 0 ? d->max_kv_len : 0, d->head_dim);
+  if (st == SIMSD_OK) st = check_fp4_cache("rotary_append_fp4", c, d->num_tokens > 0 ? d->max_kv_len : 0, d->head_dim / 32);
   if (st != SIMSD_OK) return st;
   const int64_t tokens = d->page_size > 0 ? d->page_size : d->max_kv_len;
   if (!apart(tokens, d->num_kv_heads, d->cache_stride_token, d->cache_stride_head, d->head_dim / 2) ||
@@ -316,7 +315,7 @@ simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const simsd_fp4_ca
   }
   simsd_status st = check_code_strides("fp4_values", d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head);
   const bool some = d->num > 0 && d->tokens > 0 && d->num_kv_heads > 0;
-  if (st == SIMSD_OK) st = check_fp4_cache("fp4_values", c, some, d->head_dim);
+  if (st == SIMSD_OK) st = check_fp4_cache("fp4_values", c, some, 1);
   if (st != SIMSD_OK || !some) return st;
   if (!k_out && !v_out) return fail(SIMSD_ERR_NULL_POINTER, "fp4_values: k_out or v_out is required");
   if (k_out == v_out) return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: k_out and v_out must not be the same");

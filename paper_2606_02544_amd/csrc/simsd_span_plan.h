@@ -36,8 +36,9 @@ simsd_status plan_verify_span(const simsd_attn_desc* d, bool fp4, int window, in
 // The workspace of a call with this plan.
 simsd_status check_span_workspace(const char* op, const SpanPlan& p, const void* workspace, size_t workspace_bytes);
 // The pointers and strides of a 4-bit cache of `max_len` tokens at most (whose codes'
-// strides are the descriptor's).
-simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len, int head_dim);
+// strides are the descriptor's).  Scales lie at multiples of `scales_to` bytes, a power of
+// two: a head's scales where they are read as a word, a byte where one by one.
+simsd_status check_fp4_cache(const char* op, const simsd_fp4_cache* c, int max_len, int scales_to);
 
 simsd_status plan_fp4_append(const simsd_rotary_desc* d, const simsd_fp4_cache* c);
 simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const simsd_fp4_cache* c, const void* k_out, const void* v_out);
