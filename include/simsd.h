@@ -649,7 +649,8 @@ simsd_status simsd_verify_attention_fp4(const simsd_attn_desc* desc, int32_t win
 typedef struct {
   int32_t num;                /* sequences or pages, >= 0                         */
   int32_t tokens;             /* of each, >= 0                                    */
-  int32_t num_kv_heads;       /* >= 0; num * tokens * num_kv_heads <= 2^36        */
+  int32_t num_kv_heads;       /* >= 0; num * tokens * num_kv_heads <= 2^36, and
+                                 times head_dim <= 2^37 - 8192                    */
   int32_t head_dim;           /* a multiple of 32, 32..512                        */
   int64_t cache_stride_seq;   /* of the codes, in bytes, multiples of 16          */
   int64_t cache_stride_token;

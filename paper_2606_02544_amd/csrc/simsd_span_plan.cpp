@@ -309,6 +309,9 @@ simsd_status check_fp4_values(const simsd_fp4_values_desc* d, const simsd_fp4_ca
     return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: num * tokens * num_kv_heads must be <= 2^36");
   if (d->head_dim < 32 || d->head_dim > 512 || d->head_dim % 32 != 0)
     return fail(SIMSD_ERR_UNSUPPORTED, "fp4_values: head_dim must be a multiple of 32 in [32, 512]");
+  // (A launch has fewer than 2^32 threads; 256 of them take 8192 elements.)
+  if (int64_t{d->num} * d->tokens * d->num_kv_heads * d->head_dim > (int64_t{1} << 37) - 8192)
+    return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: num * tokens * num_kv_heads * head_dim must be <= 2^37 - 8192");
   for (int64_t s : {d->cache_stride_seq, d->cache_stride_token, d->cache_stride_head}) {
     if (s < 0) return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: negative stride");
     if (s > (int64_t{1} << 48)) return fail(SIMSD_ERR_BAD_SHAPE, "fp4_values: stride beyond 2^48 bytes");

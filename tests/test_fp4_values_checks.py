@@ -37,3 +37,19 @@ def test_an_attention_reads_them_as_words(no_gpu):  # noqa: F811
     assert run() != ALIGNMENT
     for kw in (dict(k_scales=0x20002), dict(v_scales=0x20001), dict(scale_stride_token=6), dict(scale_stride_seq=1)):
         assert run(**kw) == ALIGNMENT, kw
+
+
+def test_outputs_past_one_launch(no_gpu):  # noqa: F811
+    """More than 2^37 - 8192 elements (256 GiB) of keys or values are refused by their size."""
+    def run(num, tokens, heads, d):
+        desc = Fp4ValuesDesc(num=num, tokens=tokens, num_kv_heads=heads, head_dim=d, cache_stride_seq=0, cache_stride_token=0,
+                             cache_stride_head=0)
+        cache = Fp4Pointers(0x10000, 0x20000, 0x30000, 0x40000, 0, 0, 0)
+        return binding.lib().simsd_fp4_values(ctypes.byref(desc), ctypes.byref(cache), FAKE, ctypes.c_void_p(0x90000), None)
+
+    for d in range(32, 513, 32):
+        rows = (2 ** 37 - 8192) // d
+        heads = next(h for h in range(1, 4096) if rows // h < 2 ** 31)
+        tokens = rows // heads                                 # the most that are taken
+        assert run(1, tokens, heads, d) == HIP and run(1, tokens + 1, heads, d) == 2, d
+    assert run(2 ** 20, 2 ** 16, 1, 512) == 2 and run(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 32) == 2
