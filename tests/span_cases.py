@@ -4,8 +4,9 @@ tokens, or few different sequences of a verification many times over.  The shape
 the plan gives them on 256 compute units are checked on the CPU
 (tests/test_span_shapes_host.py)."""
 
-# (new, kv): blocks of every size end inside a sequence; one fits its cache, one has none new.
-LENS = [(60, 350), (1, 300), (17, 20), (33, 33), (0, 40)]
+# (new, kv): blocks of every size end inside a sequence; one fits its cache, one has none
+# new, and one has tokens before its first position, which see nothing.
+LENS = [(60, 350), (1, 300), (17, 20), (33, 33), (0, 40), (20, 7)]
 NEW = sum(n for n, _ in LENS)
 HEADS = [(16, 2), (15, 1)]
 TOKENS = [NEW, 1000, 2000, 3000, 4000, 8000, 16000]
