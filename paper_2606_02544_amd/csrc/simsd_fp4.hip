@@ -15,6 +15,7 @@ namespace {
 //
 // Keys are turned in fp64 and rounded once: their fp32 value on the way is rounded to
 // odd, so that the code is the nearest to the turned key, as if it had not been there.
+// (The angle, position * freq in turns, is three roundings off: 3.4e-16 of itself.)
 // (An fp32 rotation is off by 1e-7, which moves one key in ten million to the
 // next code: a step of up to a third.  The fp64 products hide behind the loads.)
 //

@@ -9,7 +9,7 @@
 // key, or, for the tile of the new slots, the temporal mask's word.
 //
 // 4 bits: a tile's codes and scales are loaded into registers a tile ahead, and made bf16
-// on the way into LDS once for all row waves: two instructions a word of codes
+// on the way into LDS once for all row waves: four instructions a word of eight codes
 // (v_cvt_scalef32_pk_bf16_fp4), which is why this kernel takes 128 or 256 rows and
 // fewer go to simsd_fp4_rows.h.
 //

@@ -81,6 +81,9 @@ static simsd_status plan(const char* op, Problem c, int cus, SpanPlan* p) {
   // 73, 52 and 60.  The estimate takes 48, 91, 388, 106 and 60: between blocks this near it
   // errs both ways, and to make it prefer 128 throughout takes four prompts' last 2048 tokens
   // of 16384 from 1939 to 2081.
+  // per_cu and the costs are those of heads of 128, the costs halved for heads of 64.  (Of
+  // those three or four work-groups fit a unit where two or three are counted here, and two
+  // of 256 rows; the estimate has not been fitted to them.)
   struct Shape { int row_waves, few, tile, rows, per_cu; double alone, full; };
   constexpr Shape kBf16[] = {{2, 0, 64, 64, 2, 0.95, 1.6}, {4, 0, 64, 128, 2, 1.4, 2.2}, {8, 0, 64, 256, 1, 1.8, 2.1}};
   constexpr Shape kFp4[] = {{0, 1, 32, 32, 3, 0.5, 1.2}, {0, 2, 32, 64, 2, 0.75, 1.3}, {4, 0, 64, 128, 2, 1.4, 2.2}, {8, 0, 64, 256, 1, 1.9, 2.1}};
