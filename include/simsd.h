@@ -624,6 +624,7 @@ simsd_status simsd_rotary_append_fp4(const simsd_rotary_desc* desc, const void* 
  * values of their codes, past bf16's range (at scales of 253 and 254, which no append
  * writes) infinite, and the arithmetic is that of bf16.  dtype (of q and out)
  * SIMSD_BF16 only (SIMSD_ERR_UNSUPPORTED); cache_stride_* in bytes, multiples of 16.
+ * kv_chunk counts tiles of 64 keys, or of 32 where a call has few rows a sequence.
  */
 size_t simsd_chunk_attention_fp4_workspace_size(const simsd_chunk_desc* desc, int32_t window,
                                                 int32_t sinks);
