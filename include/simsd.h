@@ -605,10 +605,10 @@ typedef struct {
  * simsd_rotary_append to a 4-bit cache.  A turned key is rounded once to the nearest
  * code, ties to the even one, from the rotation in fp64, which is off by 1e-15 and, for
  * its angle, 4e-16 |position * freq| of the pair's length (1.3e-11 at position 32768 and
- * frequency 1); values likewise as they are.  e is the least exponent, from -125 to 125, at which the largest of the 32 is
- * below 7 * 2^e (it is held as 6 * 2^e at most); larger ones than 6 * 2^125 are held
- * as that.  32 of which one is infinite or NaN are all held as NaN.  Queries are
- * turned as in simsd_rotary_append.
+ * frequency 1); values likewise as they are.  e is the least exponent, from -125 to 125,
+ * at which the largest of the 32 is below 7 * 2^e (it is held as 6 * 2^e at most);
+ * larger ones than 6 * 2^125 are held as that.  32 of which one is infinite or NaN are
+ * all held as NaN.  Queries are turned as in simsd_rotary_append.
  *   dtype SIMSD_BF16 and head_dim 64 or 128 only (SIMSD_ERR_UNSUPPORTED); cache
  *   strides in bytes, those of the codes multiples of 16; tokens' and heads' rows of
  *   codes and of scales apart.
